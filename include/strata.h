@@ -251,6 +251,84 @@ strata_status strata_na3d_bwd_ex(const strata_na3d_desc* desc, const strata_na3d
                                  void* dk, void* dv, void* dgate, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/* ---- projection rows into the attention's head layout (Sec. 3.2, App. B.5) --
+ * A block's projection writes one row per token (b, z, y, x), row_stride elements
+ * from the next:
+ *   q: heads * d | k: kv_heads * d | v: kv_heads * d | gate: heads * gate_dim
+ * (d = head_dim, head innermost but for its d channels).  One pass normalises and
+ * rotates the heads and writes the layout that strata_na3d_fwd(_ex) takes:
+ *   q[b, h]  = R (w_q * rms(row's q head h)),
+ *   k[b, h]  = R (w_k * rms(row's k head h / (heads / kv_heads))),
+ *   v[b, h]  = row's v head h / (heads / kv_heads),    gate[b, h] = row's gate,
+ *   rms(x) = x / sqrt(mean_e x_e^2 + eps)   (qk_norm != 0; otherwise rms(x) = x),
+ * R the StereoRoPE rotation by the phase table `cs` (float32 [B, H, W, d/2, 2];
+ * NULL: the identity).  The attention is then called with cs == NULL and without
+ * its own norm.  w_q, w_k: float32 [d] on the device, the learned scale of the norm
+ * shared by all heads, both or neither (NULL: 1); they need qk_norm.  Arithmetic in
+ * float32, one rounding to dtype. */
+typedef struct {
+  int32_t B, heads, kv_heads, Z, H, W, head_dim; /* kv_heads divides heads */
+  int32_t gate_dim;   /* gate logits per head in the rows: 0 (none), 1 or head_dim */
+  int64_t row_stride; /* elements, >= the row's width, a multiple of 8 */
+  int32_t qk_norm;
+  float eps;          /* finite, >= 0 */
+  strata_dtype dtype; /* rows, q, k, v, gate and their gradients */
+} strata_qkv_desc;
+
+/* rows: [B, Z, H, W, row_stride]; q, k, v: [B, heads, Z, H, W, head_dim]; gate:
+ * [B, heads, Z, H, W] (gate_dim 1) or the shape of q (gate_dim head_dim), NULL iff
+ * gate_dim == 0.  codes, scales: both NULL, or the 8-bit form (strata_ckpt_pack's)
+ * of the rows' first C = (heads + 2 kv_heads + (gate_dim > 1) heads) * head_dim
+ * elements, written in the same pass: codes int8 [B, Z, H, W, C], scales uint8
+ * [B, Z, H, W, C/32].  One-per-head gate logits stay out of it: `gate` itself,
+ * 1/head_dim of q, is what a caller keeps.  head_dim 32, 64 or 128; fewer than 2^28
+ * tokens.  Buffers must not overlap. */
+strata_status strata_qkv_heads(const strata_qkv_desc* desc, const void* rows, const float* wq, const float* wk,
+                               const float* cs, void* q, void* k, void* v, void* gate, int8_t* codes,
+                               uint8_t* scales, void* stream);
+
+/* The same from the 8-bit form: equal bit for bit to strata_qkv_heads on rows that
+ * hold the values of the codes.  row_stride is not used; gate must be NULL when
+ * gate_dim == 1. */
+strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* codes, const uint8_t* scales,
+                                    const float* wq, const float* wk, const float* cs, void* q, void* k, void* v,
+                                    void* gate, void* stream);
+
+/* Gradient of the rows and of w_q, w_k for upstream gradients dq, dk, dv, dgate in
+ * the head layout (the outputs of strata_na3d_bwd(_ex)).  With g = R^T dq or R^T of
+ * the sum of dk over the heads that share a key head, x the row's head, y = rms(x):
+ *   dw_e = sum over tokens and heads of g_e y_e,
+ *   dx = r (u - y mean_e(u_e y_e)),  u = w * g,  r = (mean_e x_e^2 + eps)^(-1/2)
+ * (dx = g without qk_norm); v takes the sum of its dv, the gate its dgate.
+ * The rows' values come from `rows` (codes and scales NULL) or from the 8-bit form
+ * (rows NULL): then the gradient is the one at the values the codes stand for.
+ * drows: [B, Z, H, W, row_stride], elements behind the row's width left as they
+ * were.  dwq, dwk: float32 [head_dim], written, NULL iff the weights are.  Sums in
+ * float32 in a fixed order (deterministic); one rounding to dtype.  workspace: at
+ * least strata_qkv_heads_bwd_workspace_size(desc) bytes of device memory with
+ * weights, else it may be NULL.  Buffers must not overlap. */
+size_t strata_qkv_heads_bwd_workspace_size(const strata_qkv_desc* desc);
+strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows, const int8_t* codes,
+                                   const uint8_t* scales, const float* wq, const float* wk, const float* cs,
+                                   const void* dq, const void* dk, const void* dv, const void* dgate, void* drows,
+                                   float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- activations kept in 8 bits between forward and backward ----------------
+ * n elements in groups of 32 consecutive ones (the last group may be short):
+ * scales[g] = s, a biased exponent, and codes[i] with the value codes[i] * 2^(s - 133).
+ * With A the group's largest magnitude, 2^(s - 133) is the smallest power of two for
+ * which A rounds to at most 127 steps, and at least 2^-126 (s >= 7); codes are
+ * rounded to nearest, ties to even: the error of an element is at most half a step,
+ * A/127, and the rms error of normal data about 0.9 % of its standard deviation.
+ * At s = 254 (A >= 1.992 * 2^127) codes are clamped to +-127.  A group with an
+ * infinity or a NaN has s = 255 and codes 0 and stands for 32 NaN.  Encoding is
+ * exact arithmetic; decoded values are exact in bf16 (7 bits).
+ * x: [n] of dtype; codes: int8 [n]; scales: uint8 [ceil(n / 32)]; 1 <= n < 2^40. */
+strata_status strata_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, strata_dtype dtype,
+                               void* stream);
+strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dtype,
+                                 void* stream);
+
 /* ---- a8: tile stitch S = D^-1 P^T W (App. F, Eq. stitch) -------------------
  * Regular tiling: tile t = a*ntx + b has origin (a*stride_y, b*stride_x) on the
  * face.  tiles: [nty*ntx, P, Ht, Wt, C] of dtype; window: float32 [Ht*Wt],

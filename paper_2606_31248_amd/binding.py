@@ -29,6 +29,8 @@ EXPORTS = (
     "strata_tile_blend", "strata_tile_extract", "strata_na_axis_index", "strata_wind_tile_frame", "strata_kbd_window",
     "strata_duo_pad", "strata_duo_plan_bytes", "strata_duo_plan", "strata_duo_pad_planned",
     "strata_duo_pad_vjp", "strata_na3d_fwd_stitch", "strata_tile_blend_overlap", "strata_na3d_bwd_noalloc",
+    "strata_qkv_heads", "strata_qkv_heads_ckpt", "strata_qkv_heads_bwd_workspace_size", "strata_qkv_heads_bwd",
+    "strata_ckpt_pack", "strata_ckpt_unpack",
     "strata_status_string", "strata_last_error",
 )
 
@@ -49,6 +51,23 @@ class NA3DDesc(ctypes.Structure):
 class NA3DOpts(ctypes.Structure):
     _fields_ = [("qk_norm", ctypes.c_int32), ("eps", ctypes.c_float), ("gate", ctypes.c_void_p),
                 ("gate_dim", ctypes.c_int32)]
+
+
+class QKVDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("Z", ctypes.c_int32),
+                ("H", ctypes.c_int32), ("W", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("gate_dim", ctypes.c_int32), ("row_stride", ctypes.c_int64), ("qk_norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+    @property
+    def kept(self) -> int:
+        """Elements of a row that its 8-bit form holds (all but one-per-head gate logits)."""
+        return (self.heads + 2 * self.kv_heads + (self.heads if self.gate_dim > 1 else 0)) * self.head_dim
+
+    @property
+    def width(self) -> int:
+        """Elements of a row: q, k, v and the gate's logits."""
+        return self.kept + (self.heads if self.gate_dim == 1 else 0)
 
 
 _lib = None
@@ -96,6 +115,19 @@ def load(path: str = LIB_PATH):
         f = getattr(L, name)
         f.argtypes = args
         f.restype = st
+    Q, i64, size = ctypes.POINTER(QKVDesc), ctypes.c_int64, ctypes.c_size_t
+    for name, args in {
+        "strata_qkv_heads": [Q, P, P, P, P, P, P, P, P, P, P, P],
+        "strata_qkv_heads_ckpt": [Q, P, P, P, P, P, P, P, P, P, P],
+        "strata_qkv_heads_bwd": [Q, P, P, P, P, P, P, P, P, P, P, P, P, P, P, size, P],
+        "strata_ckpt_pack": [P, i64, P, P, st, P],
+        "strata_ckpt_unpack": [P, P, i64, P, st, P],
+    }.items():
+        f = getattr(L, name)
+        f.argtypes = args
+        f.restype = st
+    L.strata_qkv_heads_bwd_workspace_size.argtypes = [Q]
+    L.strata_qkv_heads_bwd_workspace_size.restype = size
     L.strata_na3d_bwd_workspace_size.argtypes = [D]
     L.strata_na3d_bwd_workspace_size.restype = ctypes.c_size_t
     L.strata_na3d_bwd_ex_workspace_size.argtypes = [D, O]
@@ -435,3 +467,112 @@ def strata_duo_pad_vjp(grad_padded, halo, plan, grad_faces, stream=None):
     _check(load().strata_duo_pad_vjp(_ptr(grad_padded), P, n, C, int(halo), _ptr(plan),
                                      plan.numel() * plan.element_size(), _ptr(grad_faces), _dtype(grad_padded),
                                      _stream(stream)))
+
+
+# ---- projection rows and the head layout; activations in 8 bits -----------------
+
+def make_qkv_desc(B, heads, Z, H, W, head_dim, dtype: int, kv_heads: Optional[int] = None, gate_dim: int = 0,
+                  row_stride: Optional[int] = None, qk_norm: bool = True, eps: float = 1e-6) -> QKVDesc:
+    """Rows [q | k | v | gate] of B x Z x H x W tokens.  kv_heads: key and value heads, each shared by
+    heads / kv_heads query heads (default: heads); row_stride: elements from one row to the next
+    (default: the row's width in whole 16-byte pieces of bf16)."""
+    d = QKVDesc(B, heads, heads if kv_heads is None else kv_heads, Z, H, W, head_dim, gate_dim, 0, int(bool(qk_norm)),
+                float(eps), int(dtype))
+    d.row_stride = (d.width + 7) // 8 * 8 if row_stride is None else row_stride
+    return d
+
+
+def _on(dev, stream):
+    """The stream for tensors on `dev`: `stream`, or dev's current one.  The launch goes to the
+    calling thread's device, which therefore has to be theirs."""
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"the tensors are on {dev}, the stream is on {stream.device}")
+    return _stream(stream)
+
+
+def _check_qkv(desc: QKVDesc, heads: dict, rows: dict, codes, scales, gate_name, weights: dict, cs):
+    """The head-layout tensors, the row tensors and codes/scales that are given, w/dw [head_dim] and cs."""
+    dt = _torch_dtype(desc.dtype)
+    grid = (desc.B, desc.Z, desc.H, desc.W)
+    shape = (desc.B, desc.heads, desc.Z, desc.H, desc.W, desc.head_dim)
+    first = next(iter(heads))
+    _need(first, heads[first], shape, dt)
+    dev = heads[first].device
+    for name, t in heads.items():
+        if name != gate_name:
+            _like(name, t, shape, dt, dev)
+        elif t is not None:
+            _like(name, t, shape if desc.gate_dim > 1 else shape[:-1], dt, dev)
+    for name, t in rows.items():
+        if t is not None:
+            _like(name, t, grid + (desc.row_stride,), dt, dev)
+    if codes is not None:
+        _like("codes", codes, grid + (desc.kept,), torch.int8, dev)
+    if scales is not None:
+        _like("scales", scales, grid + (desc.kept // 32,), torch.uint8, dev)
+    for name, t in weights.items():
+        if t is not None:
+            _like(name, t, (desc.head_dim,), torch.float32, dev)
+    if cs is not None:
+        _like("cs", cs, (desc.B, desc.H, desc.W, desc.head_dim // 2, 2), torch.float32, dev)
+    return dev
+
+
+def strata_qkv_heads(desc: QKVDesc, rows, wq, wk, cs, q, k, v, gate=None, codes=None, scales=None, stream=None):
+    """Rows [B, Z, H, W, row_stride] -> q, k (normalised, scaled, rotated), v and gate in the head layout;
+    with codes and scales also the rows' 8-bit form."""
+    if rows is None:
+        raise ValueError("rows: a tensor is required")
+    dev = _check_qkv(desc, dict(q=q, k=k, v=v, gate=gate), dict(rows=rows), codes, scales, "gate", dict(wq=wq, wk=wk), cs)
+    _check(load().strata_qkv_heads(ctypes.byref(desc), _ptr(rows), _ptr(wq), _ptr(wk), _ptr(cs), _ptr(q), _ptr(k),
+                                   _ptr(v), _ptr(gate), _ptr(codes), _ptr(scales), _on(dev, stream)))
+
+
+def strata_qkv_heads_ckpt(desc: QKVDesc, codes, scales, wq, wk, cs, q, k, v, gate=None, stream=None):
+    """strata_qkv_heads from the 8-bit form (gate: only with a logit per channel)."""
+    dev = _check_qkv(desc, dict(q=q, k=k, v=v, gate=gate), {}, codes, scales, "gate", dict(wq=wq, wk=wk), cs)
+    _check(load().strata_qkv_heads_ckpt(ctypes.byref(desc), _ptr(codes), _ptr(scales), _ptr(wq), _ptr(wk), _ptr(cs),
+                                        _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _on(dev, stream)))
+
+
+def strata_qkv_heads_bwd_workspace_size(desc: QKVDesc) -> int:
+    return int(load().strata_qkv_heads_bwd_workspace_size(ctypes.byref(desc)))
+
+
+def strata_qkv_heads_bwd(desc: QKVDesc, rows, codes, scales, wq, wk, cs, dq, dk, dv, dgate, drows, dwq, dwk,
+                         workspace, stream=None):
+    """Gradient of the rows (and of wq, wk) for dq, dk, dv, dgate; the rows' values from `rows` or from their
+    8-bit form (the other None)."""
+    if drows is None:
+        raise ValueError("drows: a tensor is required")
+    dev = _check_qkv(desc, dict(dq=dq, dk=dk, dv=dv, dgate=dgate), dict(rows=rows, drows=drows), codes, scales,
+                     "dgate", dict(wq=wq, wk=wk, dwq=dwq, dwk=dwk), cs)
+    _need("workspace", workspace, device=dev, optional=True)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().strata_qkv_heads_bwd(ctypes.byref(desc), _ptr(rows), _ptr(codes), _ptr(scales), _ptr(wq), _ptr(wk),
+                                       _ptr(cs), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dgate), _ptr(drows), _ptr(dwq),
+                                       _ptr(dwk), _ptr(workspace), nbytes, _on(dev, stream)))
+
+
+def _check_ckpt(x, codes, scales):
+    _need("x", x)
+    _need("codes", codes, None, torch.int8, x.device)
+    _need("scales", scales, None, torch.uint8, x.device)
+    n = x.numel()
+    if codes.numel() != n or scales.numel() != (n + 31) // 32:
+        raise ValueError(f"codes, scales: {codes.numel()} and {scales.numel()} elements, expected {n} and {(n + 31) // 32}")
+    return n
+
+
+def strata_ckpt_pack(x, codes, scales, stream=None):
+    """x (any shape) into 8 bits: codes int8 of as many elements, scales uint8, one per 32 consecutive ones."""
+    n = _check_ckpt(x, codes, scales)
+    _check(load().strata_ckpt_pack(_ptr(x), n, _ptr(codes), _ptr(scales), _dtype(x), _on(x.device, stream)))
+
+
+def strata_ckpt_unpack(codes, scales, x, stream=None):
+    """The values of codes and scales into x."""
+    n = _check_ckpt(x, codes, scales)
+    _check(load().strata_ckpt_unpack(_ptr(codes), _ptr(scales), n, _ptr(x), _dtype(x), _on(x.device, stream)))

@@ -310,6 +310,54 @@ static strata_status na3d_bwd_noalloc_impl(const strata_na3d_desc* desc, const v
                          reinterpret_cast<char*>(ws), (hipStream_t)stream);
 }
 
+// Sizes of a row and of the tokens; *a gets what does not depend on the call.
+static strata_status check_qkv(const strata_qkv_desc* d, bool with_rows, QkvArgs* a) {
+  REQUIRE(d, "qkv desc: null pointer");
+  REQUIRE(d->B > 0 && d->heads > 0 && d->kv_heads > 0 && d->Z > 0 && d->H > 0 && d->W > 0 && d->head_dim > 0,
+          "qkv desc: every size must be positive (B=%d heads=%d kv_heads=%d Z=%d H=%d W=%d head_dim=%d)", d->B,
+          d->heads, d->kv_heads, d->Z, d->H, d->W, d->head_dim);
+  REQUIRE(d->heads % d->kv_heads == 0, "qkv desc: kv_heads %d does not divide heads %d", d->kv_heads, d->heads);
+  REQUIRE(d->gate_dim == 0 || d->gate_dim == 1 || d->gate_dim == d->head_dim,
+          "qkv desc: gate_dim must be 0, 1 or head_dim (%d), got %d", d->head_dim, d->gate_dim);
+  REQUIRE(d->dtype == STRATA_F32 || d->dtype == STRATA_BF16, "qkv desc: unknown dtype %d", (int)d->dtype);
+  REQUIRE(!d->qk_norm || (isfinite(d->eps) && d->eps >= 0.f), "qkv desc: eps must be finite and >= 0");
+  if (d->head_dim != 32 && d->head_dim != 64 && d->head_dim != 128)
+    return set_error(STRATA_ERR_UNSUPPORTED, "head_dim %d not supported (32, 64 or 128)", d->head_dim);
+  const int64_t slices = (int64_t)d->heads + 2 * (int64_t)d->kv_heads + (d->gate_dim > 1 ? d->heads : 0);
+  REQUIRE(slices <= 65535, "qkv desc: %lld heads in a row, more than 65535", (long long)slices);
+  const int64_t kept = slices * d->head_dim, width = kept + (d->gate_dim == 1 ? d->heads : 0);
+  REQUIRE(!with_rows || (d->row_stride >= width && d->row_stride % 8 == 0),
+          "qkv desc: row_stride %lld must be a multiple of 8 and at least the row's %lld elements",
+          (long long)d->row_stride, (long long)width);
+  // a launch takes 2^24 blocks of 16 tokens (head_dim 128); rows and heads of that many exceed a card
+  const int64_t most = (int64_t)1 << 28, zh = (int64_t)d->Z * d->H;
+  REQUIRE(zh < most && zh * d->W < most && zh * d->W * d->B < most, "qkv desc: 2^28 tokens or more");
+  const int64_t tokens = zh * d->W * d->B;
+  REQUIRE(width < kMaxElems / tokens && (!with_rows || d->row_stride < kMaxElems / tokens) &&
+              (int64_t)d->heads * d->head_dim < kMaxElems / tokens,
+          "qkv desc: tensor too large");
+  a->tokens = tokens;
+  a->per_tile = zh * d->W;
+  a->hw = (int64_t)d->H * d->W;
+  a->stride = d->row_stride;
+  a->kept = kept;
+  a->heads = d->heads;
+  a->kv = d->kv_heads;
+  a->gate_dim = d->gate_dim;
+  a->slices = (int)slices;
+  a->norm = d->qk_norm != 0;
+  a->eps = d->eps;
+  return STRATA_OK;
+}
+
+static strata_status check_qkv_weights(const strata_qkv_desc* d, const float* wq, const float* wk, const float* cs) {
+  REQUIRE(!wq == !wk, "wq, wk: both or neither");
+  REQUIRE(!wq || d->qk_norm, "wq, wk: the norm's scale needs qk_norm");
+  REQUIRE(aligned16(wq) && aligned16(wk), "wq, wk: not 16-byte aligned");
+  REQUIRE(aligned16(cs), "cs: not 16-byte aligned");
+  return STRATA_OK;
+}
+
 }  // namespace strata
 
 using namespace strata;
@@ -451,6 +499,113 @@ strata_status strata_na3d_bwd_noalloc(const strata_na3d_desc* desc, const void* 
                                       const float* cs, const void* out, const void* dout, const float* lse, void* dq,
                                       void* dk, void* dv, void* stream) {
   return na3d_bwd_noalloc_impl(desc, q, k, v, cs, out, dout, lse, dq, dk, dv, stream);
+}
+
+strata_status strata_qkv_heads(const strata_qkv_desc* desc, const void* rows, const float* wq, const float* wk,
+                               const float* cs, void* q, void* k, void* v, void* gate, int8_t* codes,
+                               uint8_t* scales, void* stream) {
+  QkvArgs a;
+  strata_status st = check_qkv(desc, true, &a);
+  if (st != STRATA_OK) return st;
+  st = check_qkv_weights(desc, wq, wk, cs);
+  if (st != STRATA_OK) return st;
+  REQUIRE_PTR(rows);
+  REQUIRE_PTR(q);
+  REQUIRE_PTR(k);
+  REQUIRE_PTR(v);
+  REQUIRE(!gate == !desc->gate_dim, "gate: needed with gate_dim and NULL without");
+  REQUIRE(aligned16(gate), "gate: not 16-byte aligned");
+  REQUIRE(!codes == !scales, "codes, scales: both or neither");
+  REQUIRE(aligned16(codes) && aligned16(scales), "codes, scales: not 16-byte aligned");
+  a.rows = rows, a.wq = wq, a.wk = wk, a.cs = cs;
+  a.q = q, a.k = k, a.v = v, a.gate = gate;
+  a.out_codes = codes, a.out_scales = scales;
+  launch_qkv_heads(a, desc->head_dim, desc->dtype, (hipStream_t)stream);
+  return check_launch("strata_qkv_heads");
+}
+
+strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* codes, const uint8_t* scales,
+                                    const float* wq, const float* wk, const float* cs, void* q, void* k, void* v,
+                                    void* gate, void* stream) {
+  QkvArgs a;
+  strata_status st = check_qkv(desc, false, &a);
+  if (st != STRATA_OK) return st;
+  st = check_qkv_weights(desc, wq, wk, cs);
+  if (st != STRATA_OK) return st;
+  REQUIRE_PTR(codes);
+  REQUIRE_PTR(scales);
+  REQUIRE_PTR(q);
+  REQUIRE_PTR(k);
+  REQUIRE_PTR(v);
+  REQUIRE(!gate == (desc->gate_dim < 2), "gate: in the 8-bit form with gate_dim == head_dim only");
+  REQUIRE(aligned16(gate), "gate: not 16-byte aligned");
+  a.codes = codes, a.scales = scales, a.wq = wq, a.wk = wk, a.cs = cs;
+  a.q = q, a.k = k, a.v = v, a.gate = gate;
+  launch_qkv_heads(a, desc->head_dim, desc->dtype, (hipStream_t)stream);
+  return check_launch("strata_qkv_heads_ckpt");
+}
+
+size_t strata_qkv_heads_bwd_workspace_size(const strata_qkv_desc* desc) {
+  QkvArgs a;
+  if (check_qkv(desc, true, &a) != STRATA_OK || !a.norm) return 0;
+  return (qkv_bwd_partial_bytes(a, desc->head_dim) + 255) & ~(size_t)255;
+}
+
+strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows, const int8_t* codes,
+                                   const uint8_t* scales, const float* wq, const float* wk, const float* cs,
+                                   const void* dq, const void* dk, const void* dv, const void* dgate, void* drows,
+                                   float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream) {
+  QkvArgs a;
+  strata_status st = check_qkv(desc, true, &a);
+  if (st != STRATA_OK) return st;
+  st = check_qkv_weights(desc, wq, wk, cs);
+  if (st != STRATA_OK) return st;
+  REQUIRE(!codes == !scales, "codes, scales: both or neither");
+  REQUIRE(!rows != !codes, "rows, codes: exactly one of them holds the rows");
+  REQUIRE(aligned16(rows) && aligned16(codes) && aligned16(scales), "rows, codes, scales: not 16-byte aligned");
+  REQUIRE_PTR(dq);
+  REQUIRE_PTR(dk);
+  REQUIRE_PTR(dv);
+  REQUIRE_PTR(drows);
+  REQUIRE(!dgate == !desc->gate_dim, "dgate: needed with gate_dim and NULL without");
+  REQUIRE(aligned16(dgate), "dgate: not 16-byte aligned");
+  REQUIRE(!dwq == !wq && !dwk == !wk, "dwq, dwk: needed with wq, wk and NULL without");
+  if (wq) {
+    REQUIRE(aligned16(dwq) && aligned16(dwk), "dwq, dwk: not 16-byte aligned");
+    const size_t need = qkv_bwd_partial_bytes(a, desc->head_dim);
+    if (!workspace || workspace_bytes < need)
+      return set_error(STRATA_ERR_WORKSPACE, "workspace: %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+    REQUIRE(aligned16(workspace), "workspace: not 16-byte aligned");
+    a.partial = static_cast<float*>(workspace);
+  }
+  a.rows = rows, a.codes = codes, a.scales = scales, a.wq = wq, a.wk = wk, a.cs = cs;
+  a.q = const_cast<void*>(dq), a.k = const_cast<void*>(dk), a.v = const_cast<void*>(dv);
+  a.gate = const_cast<void*>(dgate);
+  a.drows = drows;
+  launch_qkv_heads_bwd(a, desc->head_dim, desc->dtype, dwq, dwk, (hipStream_t)stream);
+  return check_launch("strata_qkv_heads_bwd");
+}
+
+strata_status strata_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, strata_dtype dtype,
+                               void* stream) {
+  REQUIRE(n > 0 && n < kMaxElems, "ckpt: need 1 <= n < 2^40 (n=%lld)", (long long)n);
+  REQUIRE(dtype == STRATA_F32 || dtype == STRATA_BF16, "ckpt: unknown dtype %d", (int)dtype);
+  REQUIRE_PTR(x);
+  REQUIRE_PTR(codes);
+  REQUIRE_PTR(scales);
+  launch_ckpt_pack(x, n, codes, scales, dtype, (hipStream_t)stream);
+  return check_launch("strata_ckpt_pack");
+}
+
+strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dtype,
+                                 void* stream) {
+  REQUIRE(n > 0 && n < kMaxElems, "ckpt: need 1 <= n < 2^40 (n=%lld)", (long long)n);
+  REQUIRE(dtype == STRATA_F32 || dtype == STRATA_BF16, "ckpt: unknown dtype %d", (int)dtype);
+  REQUIRE_PTR(codes);
+  REQUIRE_PTR(scales);
+  REQUIRE_PTR(x);
+  launch_ckpt_unpack(codes, scales, n, x, dtype, (hipStream_t)stream);
+  return check_launch("strata_ckpt_unpack");
 }
 
 static strata_status check_tiling(int32_t nty, int32_t ntx, int32_t P, int32_t Ht, int32_t Wt,

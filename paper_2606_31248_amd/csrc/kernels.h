@@ -34,6 +34,34 @@ void launch_rope_phases(const float* coords, int B, int H, int W, int head_dim, 
 void launch_rope_apply(const void* x, void* y, const float* cs, int B, int heads, int Z, int H,
                        int W, int head_dim, strata_dtype dt, int transpose, hipStream_t s);
 
+// Projection rows and the head layout (qkv_heads.hip).  A row is cut into `slices`
+// pieces of head_dim channels (heads of q, kv of k, kv of v, and with gate_dim > 1
+// heads of the gate); with gate_dim == 1 the gate's `heads` logits follow.  The
+// backward reads dq, dk, dv, dgate through q, k, v, gate.
+struct QkvArgs {
+  const void* rows = nullptr;       // or, with codes, their 8-bit form
+  const int8_t* codes = nullptr;
+  const uint8_t* scales = nullptr;
+  const float *wq = nullptr, *wk = nullptr, *cs = nullptr;
+  void *q = nullptr, *k = nullptr, *v = nullptr, *gate = nullptr;
+  int8_t* out_codes = nullptr;
+  uint8_t* out_scales = nullptr;
+  void* drows = nullptr;
+  float* partial = nullptr;         // one [2, head_dim] of weight gradients a block
+  int64_t tokens = 0, per_tile = 0, hw = 0;  // B Z H W, Z H W, H W
+  int64_t stride = 0, kept = 0;     // elements of a row, and of its 8-bit form
+  int heads = 0, kv = 0, gate_dim = 0, slices = 0, span = 0, norm = 0;
+  float eps = 0.f;
+};
+void launch_qkv_heads(QkvArgs a, int head_dim, strata_dtype dt, hipStream_t s);
+size_t qkv_bwd_partial_bytes(QkvArgs a, int head_dim);
+void launch_qkv_heads_bwd(QkvArgs a, int head_dim, strata_dtype dt, float* dwq, float* dwk, hipStream_t s);
+
+// Activations into 8 bits and back (ckpt8.hip).
+void launch_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, strata_dtype dt, hipStream_t s);
+void launch_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dt,
+                        hipStream_t s);
+
 // Any supported dtype, head_dim, window and grid, in float32 arithmetic on the
 // float32 matrix instructions; na3d_any_takes: every grid that a device can hold.
 bool na3d_any_takes(const strata_na3d_desc& d);

@@ -1,7 +1,10 @@
-"""One pass of the hot path on device tensors, as a sequence of libstrata calls.
+"""The hot path on device tensors, as sequences of libstrata calls.
 
-coordinates (Eq. 1) -> StereoRoPE phases -> neighbourhood attention forward
-with the rotation fused into the Q/K loads -> tile stitch S = D^-1 P^T W.
+One rollout pass: coordinates (Eq. 1) -> StereoRoPE phases -> neighbourhood
+attention forward with the rotation fused into the Q/K loads -> tile stitch
+S = D^-1 P^T W.  One training block, from its projection's rows to their gradient:
+``block_forward`` and ``block_backward``, with the rows and the attention's output
+kept between them as they are or in 8 bits.
 PyTorch only allocates device memory and supplies the stream.
 """
 from __future__ import annotations
@@ -47,6 +50,101 @@ def na3d_forward(q, k, v, window, scale, cs=None, out=None, lse=None):
     desc = B.desc_for(q, window, scale)
     B.strata_na3d_fwd(desc, q, k, v, cs, out, lse)
     return out
+
+
+@dataclasses.dataclass
+class BlockSaved:
+    """What block_backward needs: the rows and the attention's output, each as it was or as
+    (codes, scales), the softmax's lse and, with a gate logit per head, the gate."""
+    qkv: B.QKVDesc
+    window: tuple
+    scale: float
+    wq: Optional[torch.Tensor]
+    wk: Optional[torch.Tensor]
+    cs: Optional[torch.Tensor]
+    lse: torch.Tensor
+    rows: object
+    out: object
+    gate: Optional[torch.Tensor] = None
+
+    def nbytes(self) -> int:
+        """Bytes kept for this block, besides the weights and the phases that all blocks share."""
+        held = [self.lse, self.gate]
+        for x in (self.rows, self.out):
+            held += list(x) if isinstance(x, tuple) else [x]
+        return sum(t.numel() * t.element_size() for t in held if t is not None)
+
+
+def _heads_like(d: B.QKVDesc, rows_dtype, device):
+    """Uninitialised q, k, v and gate (None without one) of a block."""
+    shape = (d.B, d.heads, d.Z, d.H, d.W, d.head_dim)
+    new = lambda s: torch.empty(s, dtype=rows_dtype, device=device)  # noqa: E731
+    return new(shape), new(shape), new(shape), new(shape if d.gate_dim > 1 else shape[:-1]) if d.gate_dim else None
+
+
+def _attention_of(d: B.QKVDesc, window, scale, gate):
+    """Descriptor and options of the block's attention: norm and rotation are already in q and k."""
+    desc = B.make_desc(d.B, d.heads, d.Z, d.H, d.W, d.head_dim, window, scale, d.dtype)
+    return desc, B.make_opts(gate=gate) if gate is not None else None
+
+
+def block_forward(rows, qkv: B.QKVDesc, window, scale, wq=None, wk=None, cs=None, eight_bit: bool = False):
+    """Attention of one block from its projection's rows [B, Z, H, W, row_stride]: (out, saved).
+
+    out: [B, heads, Z, H, W, head_dim], gated by the rows' gate logits if there are any.  eight_bit: `saved`
+    holds the rows and out in 8 bits (just over half the bytes of bf16) instead of the tensors themselves."""
+    q, k, v, gate = _heads_like(qkv, rows.dtype, rows.device)
+    kept = rows
+    codes = scales = None
+    if eight_bit:
+        grid = (qkv.B, qkv.Z, qkv.H, qkv.W)
+        codes = torch.empty(grid + (qkv.kept,), dtype=torch.int8, device=rows.device)
+        scales = torch.empty(grid + (qkv.kept // 32,), dtype=torch.uint8, device=rows.device)
+        kept = (codes, scales)
+    B.strata_qkv_heads(qkv, rows, wq, wk, cs, q, k, v, gate, codes, scales)
+    desc, opts = _attention_of(qkv, window, scale, gate)
+    out = torch.empty_like(q)
+    lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+    B.strata_na3d_fwd_ex(desc, opts, q, k, v, None, out, lse)
+    held = out
+    if eight_bit:
+        held = (torch.empty(out.numel(), dtype=torch.int8, device=out.device),
+                torch.empty((out.numel() + 31) // 32, dtype=torch.uint8, device=out.device))
+        B.strata_ckpt_pack(out, *held)
+    return out, BlockSaved(qkv, tuple(window), scale, wq, wk, cs, lse, kept, held,
+                           gate if qkv.gate_dim == 1 else None)
+
+
+def block_backward(saved: BlockSaved, dout):
+    """Gradient of block_forward's out: (drows [B, Z, H, W, row_stride], dwq, dwk), zeros behind the rows' width.
+
+    From 8 bits the gradients are those of the attention at the values that the codes stand for, with the
+    lse of the values they were made from."""
+    d = saved.qkv
+    q, k, v, gate = _heads_like(d, dout.dtype, dout.device)
+    rows, codes, scales = (None, *saved.rows) if isinstance(saved.rows, tuple) else (saved.rows, None, None)
+    if codes is not None:
+        B.strata_qkv_heads_ckpt(d, codes, scales, saved.wq, saved.wk, saved.cs, q, k, v,
+                                gate if d.gate_dim > 1 else None)
+        gate = saved.gate if d.gate_dim == 1 else gate
+        out = torch.empty_like(dout)
+        B.strata_ckpt_unpack(*saved.out, out)
+    else:
+        B.strata_qkv_heads(d, rows, saved.wq, saved.wk, saved.cs, q, k, v, gate)
+        out = saved.out
+    desc, opts = _attention_of(d, saved.window, saved.scale, gate)
+    dq, dk, dv = (torch.empty_like(q) for _ in range(3))
+    dgate = None if gate is None else torch.empty_like(gate)
+    ws = torch.empty(B.strata_na3d_bwd_ex_workspace_size(desc, opts), dtype=torch.uint8, device=q.device)
+    B.strata_na3d_bwd_ex(desc, opts, q, k, v, None, out, dout, saved.lse, dq, dk, dv, dgate, ws)
+    drows = torch.empty((d.B, d.Z, d.H, d.W, d.row_stride), dtype=dout.dtype, device=dout.device)
+    if d.row_stride > d.width:
+        drows[..., d.width:] = 0
+    dwq, dwk = (None if w is None else torch.empty_like(w) for w in (saved.wq, saved.wk))
+    ws = torch.empty(B.strata_qkv_heads_bwd_workspace_size(d), dtype=torch.uint8, device=q.device)
+    B.strata_qkv_heads_bwd(d, rows, codes, scales, saved.wq, saved.wk, saved.cs, dq, dk, dv, dgate, drows, dwq, dwk,
+                           ws)
+    return drows, dwq, dwk
 
 
 def face_step(q, k, v, geom: TileGeometry, window, scale, tiling, blend_window, face_out,
