@@ -24,30 +24,48 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x) {
 
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// 8 elements at `at`, a multiple of 8: 16 bytes of bf16 or 32 of float32
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* p, int64_t at, float (&v)[8]) {
-  if (BF16) {
-    const uint4 r = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes that are touched once: past the caches' replacement, which leaves them to
+// what is read again
+__device__ __forceinline__ u32x4 load16(const void* p) {
+  return __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+}
+__device__ __forceinline__ void store16(void* p, u32x4 v) { __builtin_nontemporal_store(v, static_cast<u32x4*>(p)); }
+
+__device__ __forceinline__ void widen(u32x4 r, float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = mfma::lo_bf16(w[i]), v[2 * i + 1] = mfma::hi_bf16(w[i]);
-  } else {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-    const float4 a = q[0], b = q[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  }
+  for (int i = 0; i < 4; ++i) v[2 * i] = mfma::lo_bf16(r[i]), v[2 * i + 1] = mfma::hi_bf16(r[i]);
+}
+__device__ __forceinline__ void as_floats(u32x4 a, u32x4 b, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]), v[4 + i] = __uint_as_float(b[i]);
 }
 
+// 8 elements as they lie in memory: 16 bytes of bf16 or 32 of float32
 template <bool BF16>
-__device__ __forceinline__ void store8(void* p, int64_t at, const float (&v)[8]) {
+struct Raw8;
+template <>
+struct Raw8<true> {
+  u32x4 a;
+  __device__ __forceinline__ void load(const void* p) { a = load16(p); }
+  __device__ __forceinline__ void get(float (&v)[8]) const { widen(a, v); }
+};
+template <>
+struct Raw8<false> {
+  u32x4 a, b;
+  __device__ __forceinline__ void load(const void* p) { a = load16(p), b = load16(static_cast<const char*>(p) + 16); }
+  __device__ __forceinline__ void get(float (&v)[8]) const { as_floats(a, b, v); }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store8_stream(void* p, const float (&v)[8]) {
   if (BF16) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) =
-        make_uint4(mfma::pack2(v[0], v[1]), mfma::pack2(v[2], v[3]), mfma::pack2(v[4], v[5]), mfma::pack2(v[6], v[7]));
+    store16(p, u32x4{mfma::pack2(v[0], v[1]), mfma::pack2(v[2], v[3]), mfma::pack2(v[4], v[5]), mfma::pack2(v[6], v[7])});
   } else {
-    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-    q[0] = make_float4(v[0], v[1], v[2], v[3]);
-    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+    store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    store16(static_cast<char*>(p) + 16,
+            u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
   }
 }
 
@@ -67,6 +85,11 @@ __device__ __forceinline__ void store1(void* p, int64_t at, float v) {
 // Block index in a two-dimensional grid: HIP wants gridDim.x * blockDim.x below
 // 2^32, and a card's largest activations exceed that.
 __device__ __forceinline__ int64_t block_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+inline dim3 grid_of(int64_t blocks) {
+  const int64_t y = (blocks + (1 << 20) - 1) >> 20;
+  return dim3((unsigned)((blocks + y - 1) / y), (unsigned)y);
+}
 
 // Biased exponent of the group whose largest |bits| is `top`: where 2^(E - 133)
 // would make it round to 128 steps (mantissa >= 127.5/64) the sum carries into the
@@ -103,6 +126,13 @@ __device__ __forceinline__ void decode8(uint2 c, float step, float (&v)[8]) {
   const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};  // code + 128: unsigned bytes convert in one instruction
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = ((float)((w[i >> 2] >> (8 * (i & 3))) & 255u) - 128.f) * step;
+}
+
+// Two neighbouring slices' codes between "each lane its 8 of both" and "an even lane 16 of
+// the first slice, its own and the next lane's, an odd lane 16 of the second"; its own inverse.
+__device__ __forceinline__ void swap_pair(int odd, uint2& first, uint2& second) {
+  const uint32_t gx = dpp<kSwap1>(odd ? first.x : second.x), gy = dpp<kSwap1>(odd ? first.y : second.y);
+  (odd ? first : second) = make_uint2(gx, gy);
 }
 
 // largest |bits| of the quad's 32 values

@@ -17,7 +17,9 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const void* __restrict__
   const int64_t at = i * 8;
   float v[8];
   if (at + 8 <= n) {
-    load8<BF16>(x, at, v);
+    Raw8<BF16> raw;
+    raw.load(static_cast<const char*>(x) + at * (BF16 ? 2 : 4));
+    raw.get(v);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = at + j < n ? load1<BF16>(x, at + j) : 0.f;
@@ -45,22 +47,18 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const int8_t* __restri
   float v[8];
   if (at + 8 <= n) {
     decode8(*reinterpret_cast<const uint2*>(codes + at), step, v);
-    store8<BF16>(x, at, v);
+    store8_stream<BF16>(static_cast<char*>(x) + at * (BF16 ? 2 : 4), v);
   } else {
     for (int j = 0; at + j < n; ++j) store1<BF16>(x, at + j, (float)codes[at + j] * step);
   }
 }
 
-static dim3 grid_of(int64_t n) {
-  const int64_t blocks = (n + 8 * kThreads - 1) / (8 * kThreads);
-  const int64_t y = (blocks + (1 << 20) - 1) >> 20;
-  return dim3((unsigned)((blocks + y - 1) / y), (unsigned)y);
-}
+static dim3 blocks_for(int64_t n) { return grid_of((n + 8 * kThreads - 1) / (8 * kThreads)); }
 
 }  // namespace ckpt8
 
 void launch_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, strata_dtype dt, hipStream_t s) {
-  const dim3 grid = ckpt8::grid_of(n);
+  const dim3 grid = ckpt8::blocks_for(n);
   if (dt == STRATA_BF16)
     hipLaunchKernelGGL(ckpt8::pack_kernel<true>, grid, dim3(ckpt8::kThreads), 0, s, x, n, codes, scales);
   else
@@ -69,7 +67,7 @@ void launch_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, 
 
 void launch_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dt,
                         hipStream_t s) {
-  const dim3 grid = ckpt8::grid_of(n);
+  const dim3 grid = ckpt8::blocks_for(n);
   if (dt == STRATA_BF16)
     hipLaunchKernelGGL(ckpt8::unpack_kernel<true>, grid, dim3(ckpt8::kThreads), 0, s, codes, scales, n, x);
   else

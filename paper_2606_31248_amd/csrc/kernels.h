@@ -38,6 +38,9 @@ void launch_rope_apply(const void* x, void* y, const float* cs, int B, int heads
 // pieces of head_dim channels (heads of q, kv of k, kv of v, and with gate_dim > 1
 // heads of the gate); with gate_dim == 1 the gate's `heads` logits follow.  The
 // backward reads dq, dk, dv, dgate through q, k, v, gate.
+struct FastDiv {
+  uint32_t mul = 0, shift = 0;  // n / d = mulhi(n, mul) >> shift for n < 2^31; mul = 0: d = 1
+};
 struct QkvArgs {
   const void* rows = nullptr;       // or, with codes, their 8-bit form
   const int8_t* codes = nullptr;
@@ -50,8 +53,12 @@ struct QkvArgs {
   float* partial = nullptr;         // one [2, head_dim] of weight gradients a block
   int64_t tokens = 0, per_tile = 0, hw = 0;  // B Z H W, Z H W, H W
   int64_t stride = 0, kept = 0;     // elements of a row, and of its 8-bit form
-  int heads = 0, kv = 0, gate_dim = 0, slices = 0, span = 0, norm = 0;
+  int heads = 0, kv = 0, gate_dim = 0, slices = 0, norm = 0;
   float eps = 0.f;
+  // the launch: waves = groups of heads x (token tiles / steps), heads / kv
+  uint32_t waves = 0, groups = 0, tiles = 0, steps = 1;
+  int share = 1;
+  FastDiv by_groups, by_tile, by_hw;
 };
 void launch_qkv_heads(QkvArgs a, int head_dim, strata_dtype dt, hipStream_t s);
 size_t qkv_bwd_partial_bytes(QkvArgs a, int head_dim);
