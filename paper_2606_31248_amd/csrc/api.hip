@@ -548,7 +548,7 @@ strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* c
 size_t strata_qkv_heads_bwd_workspace_size(const strata_qkv_desc* desc) {
   QkvArgs a;
   if (check_qkv(desc, true, &a) != STRATA_OK || !a.norm) return 0;
-  return (qkv_bwd_partial_bytes(a, desc->head_dim) + 255) & ~(size_t)255;
+  return (qkv_bwd_partial_bytes(a, desc->head_dim, desc->dtype) + 255) & ~(size_t)255;
 }
 
 strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows, const int8_t* codes,
@@ -572,7 +572,7 @@ strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows
   REQUIRE(!dwq == !wq && !dwk == !wk, "dwq, dwk: needed with wq, wk and NULL without");
   if (wq) {
     REQUIRE(aligned16(dwq) && aligned16(dwk), "dwq, dwk: not 16-byte aligned");
-    const size_t need = qkv_bwd_partial_bytes(a, desc->head_dim);
+    const size_t need = qkv_bwd_partial_bytes(a, desc->head_dim, desc->dtype);
     if (!workspace || workspace_bytes < need)
       return set_error(STRATA_ERR_WORKSPACE, "workspace: %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
     REQUIRE(aligned16(workspace), "workspace: not 16-byte aligned");

@@ -42,20 +42,40 @@ __device__ __forceinline__ void as_floats(u32x4 a, u32x4 b, float (&v)[8]) {
   for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]), v[4 + i] = __uint_as_float(b[i]);
 }
 
-// 8 elements as they lie in memory: 16 bytes of bf16 or 32 of float32
+// 8 elements as they lie in memory: 16 bytes of bf16 or 32 of float32.  STREAM: past
+// the caches' replacement; bf16 alone, since the two halves of a lane's float32 meet in
+// the same cache lines.
 template <bool BF16>
 struct Raw8;
 template <>
 struct Raw8<true> {
   u32x4 a;
-  __device__ __forceinline__ void load(const void* p) { a = load16(p); }
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const void* p) {
+    a = STREAM ? load16(p) : *static_cast<const u32x4*>(p);
+  }
   __device__ __forceinline__ void get(float (&v)[8]) const { widen(a, v); }
+  // elements [at, n) of less than 8, then zeros
+  __device__ __forceinline__ void load_part(const void* p, int64_t at, int64_t n) {
+    const uint16_t* q = static_cast<const uint16_t*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      a[j] = (at + 2 * j < n ? q[at + 2 * j] : 0u) | (at + 2 * j + 1 < n ? (uint32_t)q[at + 2 * j + 1] << 16 : 0u);
+  }
 };
 template <>
 struct Raw8<false> {
   u32x4 a, b;
-  __device__ __forceinline__ void load(const void* p) { a = load16(p), b = load16(static_cast<const char*>(p) + 16); }
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const void* p) {
+    a = static_cast<const u32x4*>(p)[0], b = static_cast<const u32x4*>(p)[1];
+  }
   __device__ __forceinline__ void get(float (&v)[8]) const { as_floats(a, b, v); }
+  __device__ __forceinline__ void load_part(const void* p, int64_t at, int64_t n) {
+    const uint32_t* q = static_cast<const uint32_t*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = at + j < n ? q[at + j] : 0u, b[j] = at + 4 + j < n ? q[at + 4 + j] : 0u;
+  }
 };
 
 template <bool BF16>
@@ -63,15 +83,10 @@ __device__ __forceinline__ void store8_stream(void* p, const float (&v)[8]) {
   if (BF16) {
     store16(p, u32x4{mfma::pack2(v[0], v[1]), mfma::pack2(v[2], v[3]), mfma::pack2(v[4], v[5]), mfma::pack2(v[6], v[7])});
   } else {
-    store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-    store16(static_cast<char*>(p) + 16,
-            u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+    u32x4* q = static_cast<u32x4*>(p);
+    q[0] = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    q[1] = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
   }
-}
-
-template <bool BF16>
-__device__ __forceinline__ float load1(const void* p, int64_t at) {
-  return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[at]) : static_cast<const float*>(p)[at];
 }
 
 template <bool BF16>
@@ -105,27 +120,62 @@ __device__ __forceinline__ float step_of(uint32_t e) {
   return __uint_as_float(e == 255u ? 0x7FC00000u : (e - 6u) << 23);
 }
 
-// Codes of 8 values (4 bytes a word) with the inverse step 2^(133 - E): the
-// product is exact, and adding 1.5 * 2^23 rounds it to an integer, ties to even,
-// whose two's complement is the sum's low byte.
+// Codes of 8 values (4 bytes a word): v 2^(133 - E), exact, plus 1.5 * 2^23 in one
+// fused multiply-add rounds to an integer, ties to even, whose two's complement is
+// the sum's low byte.  Only E = 254 can round to 128.
 __device__ __forceinline__ uint2 encode8(const float (&v)[8], uint32_t e) {
-  if (e == 255u) return make_uint2(0u, 0u);
+  constexpr float kRound = 12582912.f;
   const float inv = __uint_as_float((260u - e) << 23);
   uint32_t b[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    b[i] = __float_as_uint(__builtin_amdgcn_fmed3f(v[i] * inv, -127.f, 127.f) + 12582912.f);
-  auto pack = [](uint32_t p, uint32_t q, uint32_t r, uint32_t s) {
-    return (p & 255u) | (q & 255u) << 8 | (r & 255u) << 16 | s << 24;
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], inv, kRound));
+  if (e >= 254u) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      b[i] = e == 255u ? 0u : __float_as_uint(__builtin_amdgcn_fmed3f(v[i] * inv, -127.f, 127.f) + kRound);
+  }
+  auto pack = [](uint32_t p, uint32_t q, uint32_t r, uint32_t s) {  // the low byte of each
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(s, r, 0x0C0C0400u), __builtin_amdgcn_perm(q, p, 0x0C0C0400u),
+                                 0x05040100u);
   };
   return make_uint2(pack(b[0], b[1], b[2], b[3]), pack(b[4], b[5], b[6], b[7]));
 }
 
+// code + 128 of the i-th of 8 codes whose words were flipped by 0x80808080: unsigned
+// bytes convert in one instruction
+__device__ __forceinline__ float code_up(uint2 flipped, int i) {
+  return (float)(((i < 4 ? flipped.x : flipped.y) >> (8 * (i & 3))) & 255u);
+}
+__device__ __forceinline__ uint2 flip(uint2 c) { return make_uint2(c.x ^ 0x80808080u, c.y ^ 0x80808080u); }
+
 // 8 codes -> values
 __device__ __forceinline__ void decode8(uint2 c, float step, float (&v)[8]) {
-  const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};  // code + 128: unsigned bytes convert in one instruction
+  const uint2 w = flip(c);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = ((float)((w[i >> 2] >> (8 * (i & 3))) & 255u) - 128.f) * step;
+  for (int i = 0; i < 8; ++i) v[i] = (code_up(w, i) - 128.f) * step;
+}
+
+// 8 codes -> values times f, rounded once: (code + 128) F - 128 F with F = step f.
+// F has to stay below 2^120: a step of 2^121 only with f = 0.
+__device__ __forceinline__ void decode8_times(uint2 c, float step, float f, float (&v)[8]) {
+  const uint2 w = flip(c);
+  const float m = step * f, off = -128.f * m;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = fmaf(code_up(w, i), m, off);
+}
+
+// Sum of the squares of 8 codes, below 2^17 and so exact, as the sum of their values'
+// squares over step^2 is in float32
+__device__ __forceinline__ float code_squares(uint2 c) {
+  return (float)__builtin_amdgcn_sdot4((int)c.x, (int)c.x, __builtin_amdgcn_sdot4((int)c.y, (int)c.y, 0, false), false);
+}
+
+// OR over the quads of LANES neighbouring lanes
+template <int LANES>
+__device__ __forceinline__ uint32_t quads_or(uint32_t x) {
+  if (LANES >= 8) x |= dpp<kMirror8>(x);
+  if (LANES >= 16) x |= dpp<kMirror16>(x);
+  return x;
 }
 
 // Two neighbouring slices' codes between "each lane its 8 of both" and "an even lane 16 of
@@ -135,11 +185,21 @@ __device__ __forceinline__ void swap_pair(int odd, uint2& first, uint2& second) 
   (odd ? first : second) = make_uint2(gx, gy);
 }
 
-// largest |bits| of the quad's 32 values
-__device__ __forceinline__ uint32_t group_top(const float (&v)[8]) {
+// largest |bits|, as float32, of the quad's 32 values: bf16 as they lie, two to a word
+__device__ __forceinline__ uint32_t group_top(const Raw8<true>& raw) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  auto half = [](uint32_t w) { return __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu); };
+  const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(half(raw.a[0]), half(raw.a[1])),
+                                            __builtin_elementwise_max(half(raw.a[2]), half(raw.a[3])));
+  uint32_t t = (uint32_t)(m.x > m.y ? m.x : m.y) << 16;
+  t = umax(t, dpp<kSwap1>(t));
+  return umax(t, dpp<kSwap2>(t));
+}
+
+__device__ __forceinline__ uint32_t group_top(const Raw8<false>& raw) {
   uint32_t t = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) t = umax(t, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < 4; ++i) t = umax(t, umax(raw.a[i] & 0x7FFFFFFFu, raw.b[i] & 0x7FFFFFFFu));
   t = umax(t, dpp<kSwap1>(t));
   return umax(t, dpp<kSwap2>(t));
 }

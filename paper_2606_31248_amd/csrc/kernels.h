@@ -55,13 +55,17 @@ struct QkvArgs {
   int64_t stride = 0, kept = 0;     // elements of a row, and of its 8-bit form
   int heads = 0, kv = 0, gate_dim = 0, slices = 0, norm = 0;
   float eps = 0.f;
-  // the launch: waves = groups of heads x (token tiles / steps), heads / kv
-  uint32_t waves = 0, groups = 0, tiles = 0, steps = 1;
-  int share = 1;
-  FastDiv by_groups, by_tile, by_hw;
+  // the launch: a wave takes every stride_tiles-th token tile of one group of heads.  Forward: waves =
+  // groups x stride_tiles; backward: the groups of q and k in the first norm_blocks blocks, the `rest` after them.
+  uint32_t waves = 0, groups = 0, rest = 0, tiles = 0, stride_tiles = 0;
+  int64_t blocks = 0, norm_blocks = 0;
+  int groups_q = 0, groups_k = 0;
+  int near = 0;              // log2 of a token's heads that lie beside each other in a wave
+  int share = 1;             // heads / kv
+  FastDiv by_groups, by_rest, by_tile, by_hw;
 };
 void launch_qkv_heads(QkvArgs a, int head_dim, strata_dtype dt, hipStream_t s);
-size_t qkv_bwd_partial_bytes(QkvArgs a, int head_dim);
+size_t qkv_bwd_partial_bytes(QkvArgs a, int head_dim, strata_dtype dt);
 void launch_qkv_heads_bwd(QkvArgs a, int head_dim, strata_dtype dt, float* dwq, float* dwk, hipStream_t s);
 
 // Activations into 8 bits and back (ckpt8.hip).
