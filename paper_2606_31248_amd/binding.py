@@ -482,42 +482,50 @@ def make_qkv_desc(B, heads, Z, H, W, head_dim, dtype: int, kv_heads: Optional[in
     return d
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _on(dev, stream):
     """The stream for tensors on `dev`: `stream`, or dev's current one.  The launch goes to the
     calling thread's device, which therefore has to be theirs."""
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
-    if stream is not None and stream.device != dev:
+    index = _current_device()
+    if dev.index != index:
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{index}")
+    if stream is None:
+        return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if stream.device != dev:
         raise ValueError(f"the tensors are on {dev}, the stream is on {stream.device}")
-    return _stream(stream)
+    return stream.cuda_stream
 
 
-def _check_qkv(desc: QKVDesc, heads: dict, rows: dict, codes, scales, gate_name, weights: dict, cs):
-    """The head-layout tensors, the row tensors and codes/scales that are given, w/dw [head_dim] and cs."""
+def _at(name: str, t, shape, dtype, device):
+    """The address of a tensor of exactly this shape, dtype and device, or None for None: one pass over the
+    conditions, and _need for the message where one fails."""
+    if t is None:
+        return None
+    if not (type(t) is torch.Tensor and t.shape == shape and t.dtype is dtype and t.device == device
+            and t.is_contiguous()):
+        _need(name, t, shape, dtype, device)
+    return t.data_ptr()
+
+
+def _qkv_common(desc: QKVDesc, name: str, q, wq, wk, cs):
+    """(dtype, grid, head-layout shape, device of q, addresses of wq, wk and cs)"""
     dt = _torch_dtype(desc.dtype)
-    grid = (desc.B, desc.Z, desc.H, desc.W)
-    shape = (desc.B, desc.heads, desc.Z, desc.H, desc.W, desc.head_dim)
-    first = next(iter(heads))
-    _need(first, heads[first], shape, dt)
-    dev = heads[first].device
-    for name, t in heads.items():
-        if name != gate_name:
-            _like(name, t, shape, dt, dev)
-        elif t is not None:
-            _like(name, t, shape if desc.gate_dim > 1 else shape[:-1], dt, dev)
-    for name, t in rows.items():
-        if t is not None:
-            _like(name, t, grid + (desc.row_stride,), dt, dev)
-    if codes is not None:
-        _like("codes", codes, grid + (desc.kept,), torch.int8, dev)
-    if scales is not None:
-        _like("scales", scales, grid + (desc.kept // 32,), torch.uint8, dev)
-    for name, t in weights.items():
-        if t is not None:
-            _like(name, t, (desc.head_dim,), torch.float32, dev)
-    if cs is not None:
-        _like("cs", cs, (desc.B, desc.H, desc.W, desc.head_dim // 2, 2), torch.float32, dev)
-    return dev
+    B, Z, H, W, d = desc.B, desc.Z, desc.H, desc.W, desc.head_dim
+    shape = (B, desc.heads, Z, H, W, d)
+    _need(name, q, shape, dt)
+    dev = q.device
+    return (dt, (B, Z, H, W), shape, dev, _at("wq", wq, (d,), torch.float32, dev), _at("wk", wk, (d,), torch.float32, dev),
+            _at("cs", cs, (B, H, W, d // 2, 2), torch.float32, dev))
+
+
+def _codes_at(desc: QKVDesc, grid, dev, codes, scales):
+    if codes is None and scales is None:
+        return None, None
+    kept = desc.kept
+    return (_at("codes", codes, grid + (kept,), torch.int8, dev),
+            _at("scales", scales, grid + (kept // 32,), torch.uint8, dev))
 
 
 def strata_qkv_heads(desc: QKVDesc, rows, wq, wk, cs, q, k, v, gate=None, codes=None, scales=None, stream=None):
@@ -525,16 +533,21 @@ def strata_qkv_heads(desc: QKVDesc, rows, wq, wk, cs, q, k, v, gate=None, codes=
     with codes and scales also the rows' 8-bit form."""
     if rows is None:
         raise ValueError("rows: a tensor is required")
-    dev = _check_qkv(desc, dict(q=q, k=k, v=v, gate=gate), dict(rows=rows), codes, scales, "gate", dict(wq=wq, wk=wk), cs)
-    _check(load().strata_qkv_heads(ctypes.byref(desc), _ptr(rows), _ptr(wq), _ptr(wk), _ptr(cs), _ptr(q), _ptr(k),
-                                   _ptr(v), _ptr(gate), _ptr(codes), _ptr(scales), _on(dev, stream)))
+    dt, grid, shape, dev, w_q, w_k, table = _qkv_common(desc, "q", q, wq, wk, cs)
+    c, s = _codes_at(desc, grid, dev, codes, scales)
+    _check(load().strata_qkv_heads(
+        ctypes.byref(desc), _at("rows", rows, grid + (desc.row_stride,), dt, dev), w_q, w_k, table, q.data_ptr(),
+        _at("k", k, shape, dt, dev), _at("v", v, shape, dt, dev),
+        _at("gate", gate, shape if desc.gate_dim > 1 else shape[:-1], dt, dev), c, s, _on(dev, stream)))
 
 
 def strata_qkv_heads_ckpt(desc: QKVDesc, codes, scales, wq, wk, cs, q, k, v, gate=None, stream=None):
     """strata_qkv_heads from the 8-bit form (gate: only with a logit per channel)."""
-    dev = _check_qkv(desc, dict(q=q, k=k, v=v, gate=gate), {}, codes, scales, "gate", dict(wq=wq, wk=wk), cs)
-    _check(load().strata_qkv_heads_ckpt(ctypes.byref(desc), _ptr(codes), _ptr(scales), _ptr(wq), _ptr(wk), _ptr(cs),
-                                        _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _on(dev, stream)))
+    dt, grid, shape, dev, w_q, w_k, table = _qkv_common(desc, "q", q, wq, wk, cs)
+    c, s = _codes_at(desc, grid, dev, codes, scales)
+    _check(load().strata_qkv_heads_ckpt(
+        ctypes.byref(desc), c, s, w_q, w_k, table, q.data_ptr(), _at("k", k, shape, dt, dev), _at("v", v, shape, dt, dev),
+        _at("gate", gate, shape if desc.gate_dim > 1 else shape[:-1], dt, dev), _on(dev, stream)))
 
 
 def strata_qkv_heads_bwd_workspace_size(desc: QKVDesc) -> int:
@@ -547,32 +560,39 @@ def strata_qkv_heads_bwd(desc: QKVDesc, rows, codes, scales, wq, wk, cs, dq, dk,
     8-bit form (the other None)."""
     if drows is None:
         raise ValueError("drows: a tensor is required")
-    dev = _check_qkv(desc, dict(dq=dq, dk=dk, dv=dv, dgate=dgate), dict(rows=rows, drows=drows), codes, scales,
-                     "dgate", dict(wq=wq, wk=wk, dwq=dwq, dwk=dwk), cs)
+    dt, grid, shape, dev, w_q, w_k, table = _qkv_common(desc, "dq", dq, wq, wk, cs)
+    c, s = _codes_at(desc, grid, dev, codes, scales)
+    row, d = grid + (desc.row_stride,), (desc.head_dim,)
     _need("workspace", workspace, device=dev, optional=True)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().strata_qkv_heads_bwd(ctypes.byref(desc), _ptr(rows), _ptr(codes), _ptr(scales), _ptr(wq), _ptr(wk),
-                                       _ptr(cs), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dgate), _ptr(drows), _ptr(dwq),
-                                       _ptr(dwk), _ptr(workspace), nbytes, _on(dev, stream)))
+    _check(load().strata_qkv_heads_bwd(
+        ctypes.byref(desc), _at("rows", rows, row, dt, dev), c, s, w_q, w_k, table, dq.data_ptr(),
+        _at("dk", dk, shape, dt, dev), _at("dv", dv, shape, dt, dev),
+        _at("dgate", dgate, shape if desc.gate_dim > 1 else shape[:-1], dt, dev), _at("drows", drows, row, dt, dev),
+        _at("dwq", dwq, d, torch.float32, dev), _at("dwk", dwk, d, torch.float32, dev), _ptr(workspace), nbytes,
+        _on(dev, stream)))
 
 
-def _check_ckpt(x, codes, scales):
-    _need("x", x)
-    _need("codes", codes, None, torch.int8, x.device)
-    _need("scales", scales, None, torch.uint8, x.device)
-    n = x.numel()
-    if codes.numel() != n or scales.numel() != (n + 31) // 32:
-        raise ValueError(f"codes, scales: {codes.numel()} and {scales.numel()} elements, expected {n} and {(n + 31) // 32}")
-    return n
+def _ckpt_args(x, codes, scales):
+    """(elements, address of x, of codes, of scales)"""
+    if not (type(x) is torch.Tensor and x.is_cuda and x.is_contiguous()):
+        _need("x", x)
+    n, dev = x.numel(), x.device
+    for name, t, dt, many in (("codes", codes, torch.int8, n), ("scales", scales, torch.uint8, (n + 31) // 32)):
+        if not (type(t) is torch.Tensor and t.dtype is dt and t.device == dev and t.numel() == many
+                and t.is_contiguous()):
+            _need(name, t, None, dt, dev)
+            raise ValueError(f"{name}: {t.numel()} elements, expected {many}")
+    return n, x.data_ptr(), codes.data_ptr(), scales.data_ptr()
 
 
 def strata_ckpt_pack(x, codes, scales, stream=None):
     """x (any shape) into 8 bits: codes int8 of as many elements, scales uint8, one per 32 consecutive ones."""
-    n = _check_ckpt(x, codes, scales)
-    _check(load().strata_ckpt_pack(_ptr(x), n, _ptr(codes), _ptr(scales), _dtype(x), _on(x.device, stream)))
+    n, px, pc, ps = _ckpt_args(x, codes, scales)
+    _check(load().strata_ckpt_pack(px, n, pc, ps, _dtype(x), _on(x.device, stream)))
 
 
 def strata_ckpt_unpack(codes, scales, x, stream=None):
     """The values of codes and scales into x."""
-    n = _check_ckpt(x, codes, scales)
-    _check(load().strata_ckpt_unpack(_ptr(codes), _ptr(scales), n, _ptr(x), _dtype(x), _on(x.device, stream)))
+    n, px, pc, ps = _ckpt_args(x, codes, scales)
+    _check(load().strata_ckpt_unpack(pc, ps, n, px, _dtype(x), _on(x.device, stream)))
