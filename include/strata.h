@@ -288,7 +288,8 @@ strata_status strata_qkv_heads(const strata_qkv_desc* desc, const void* rows, co
                                uint8_t* scales, void* stream);
 
 /* The same from the 8-bit form: equal bit for bit to strata_qkv_heads on rows that
- * hold the values of the codes.  row_stride is not used; gate must be NULL when
+ * hold the values of the codes (where a head's sum of squares overflows and its norm
+ * is 0, but for the sign of that 0).  row_stride is not used; gate must be NULL when
  * gate_dim == 1. */
 strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* codes, const uint8_t* scales,
                                     const float* wq, const float* wk, const float* cs, void* q, void* k, void* v,
@@ -306,7 +307,9 @@ strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* c
  * were.  dwq, dwk: float32 [head_dim], written, NULL iff the weights are.  Sums in
  * float32 in a fixed order (deterministic); one rounding to dtype.  workspace: at
  * least strata_qkv_heads_bwd_workspace_size(desc) bytes of device memory with
- * weights, else it may be NULL.  Buffers must not overlap. */
+ * weights, else it may be NULL; calls in flight at once need one each.  Buffers must
+ * not overlap.  Rows that start on 128-byte lines (row_stride a multiple of 64 in
+ * bf16) are written fastest: others take about 1.4 times as long. */
 size_t strata_qkv_heads_bwd_workspace_size(const strata_qkv_desc* desc);
 strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows, const int8_t* codes,
                                    const uint8_t* scales, const float* wq, const float* wk, const float* cs,

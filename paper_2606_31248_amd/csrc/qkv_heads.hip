@@ -20,14 +20,15 @@ namespace qkv {
 
 using namespace ckpt8;
 
-// Waves of a block, and heads of one kind that a wave takes.  The training tile's heads
-// from codes take 560 us with 4, 600 with 2 (1 KB of codes a load); its rows 780 with 4
-// and 720 with 2; its backward 830 with 2, 890 with 4 (registers) and 910 with 1.
+// Waves of a block, and heads of one kind that a wave takes.  The training tile (8 tiles,
+// 16 heads and their gate): rows 720 us with 2 and 780 with 4; with codes 950 and 900 (the
+// exponents of 4 heads in one piece), from codes 600 and 560; the backward 850 with 2, 930
+// with 4 (registers) and 920 with 1.
 constexpr int kWaves = 4, kBwdHeads = 2;
 
 // What the forward reads and writes beside the heads
 enum Mode { kRows, kRowsToCodes, kFromCodes };
-constexpr int fwd_heads(int mode) { return mode == kFromCodes ? 4 : 2; }
+constexpr int fwd_heads(int mode) { return mode == kRows ? 2 : 4; }
 
 // The sum over the lanes that hold one head's channels.
 template <int LANES>
@@ -174,7 +175,8 @@ struct Slices {
 };
 
 // Codes.  Of two of its slices an even lane loads its own and the next lane's 8 codes
-// of the first, an odd lane the same of the second; a swap gives each lane its 8 of both.  Steps are powers of two, so that each result equals the rows' bit for bit.
+// of the first, an odd lane the same of the second; a swap gives each lane its 8 of
+// both.  Steps are powers of two, so that each result equals the rows' bit for bit.
 // A step of 2^121 makes a sum of squares infinite and the factor 0: the norm's values
 // are then 0 whatever the codes, and their step is taken as 0.
 template <bool BF16, int D, int NH, int NEAR, bool STREAM>
@@ -236,8 +238,7 @@ __device__ __forceinline__ void move_logits(const QkvArgs& a, uint32_t tile, uin
 template <bool BF16, int D, int MODE, bool STREAM>
 __global__ void __launch_bounds__(kWaves * 64) fwd_kernel(const QkvArgs a) {
   constexpr int kLanes = D / 8, kBytes = BF16 ? 2 : 4, kHeads = fwd_heads(MODE);
-  const uint32_t wave = (uint32_t)block_index() * kWaves +
-                        __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t wave = (uint32_t)block_index() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (wave >= a.waves) return;
   const uint32_t at_tile = div_by(wave, a.by_groups);
   const Work w = work_of<kHeads, kHeads, 0>(a, at_tile, (int)(wave - at_tile * a.groups));
@@ -291,7 +292,8 @@ __global__ void __launch_bounds__(kWaves * 64) fwd_kernel(const QkvArgs a) {
       if (i + 1 < kHeads && i + 1 < w.n) {
         swap_pair(odd, code[i], code[i + 1]);
         if (p.valid)
-          store16(a.out_codes + at + (i + odd) * D + 8 * (p.sub - odd), u32x4{code[i].x, code[i].y, code[i + 1].x, code[i + 1].y});
+          store16(a.out_codes + at + (i + odd) * D + 8 * (p.sub - odd),
+                  u32x4{code[i].x, code[i].y, code[i + 1].x, code[i + 1].y});
       } else if (i < w.n && p.valid) {
         *reinterpret_cast<uint2*>(a.out_codes + at + i * D + 8 * p.sub) = code[i];
       }
@@ -331,13 +333,101 @@ __device__ __forceinline__ void token_sums(float (&v)[8]) {
   if (D == 32) v[0] += __shfl_xor(v[0], 4);
 }
 
-// Blocks [0, norm_blocks) take the heads of q and k and write a row of partial weight
-// gradients each, the others those of v and the gate.
+// The gradient of a wave's slices, tile after tile: without NORM rotated back and copied,
+// with it through the norm, dw taking up the lane's part of the weight's gradient.
 // SHARED: k and v heads of several query heads, whose gradients are added; a wave then
 // takes one of them, with four of its loads in flight.
+template <bool BF16, int D, bool CODES, bool SHARED, int NEAR, bool NORM>
+__device__ __forceinline__ void backward(const QkvArgs& a, const Work& w, float (&dw)[8]) {
+  constexpr int kLanes = D / 8, kBytes = BF16 ? 2 : 4;
+  const int sub = threadIdx.x & (kLanes - 1), kind = w.kind;
+  const bool turn = kind <= kK && a.cs;
+  const float* weight = kind == kQ ? a.wq : a.wk;
+  float wt[8];
+  if (NORM && weight) load_weights(weight, sub, wt);
+  const int64_t plane = a.per_tile * D * kBytes;
+  const int share = kind == kK || kind == kV ? a.share : 1;
+  const char* from = static_cast<const char*>(kind == kQ ? a.q : kind == kK ? a.k : kind == kV ? a.v : a.gate) +
+                     (int64_t)w.h0 * share * plane;
+  for (uint32_t tile = w.tile; tile < a.tiles; tile += a.stride_tiles) {
+    const Place p = place<D, NEAR>(a, tile);
+    const char* in = from + p.b * a.heads * plane + (p.r * D + 8 * sub) * kBytes;
+    Raw8<BF16> up[kBwdHeads];
+#pragma unroll
+    for (int i = 0; i < kBwdHeads; ++i)
+      up[i].template load<true>(in + (int64_t)head_of<NEAR>(p, w, i) * share * plane);
+    Slices<BF16, D, CODES, kBwdHeads, NEAR, NEAR == 0> rows;
+    if (NORM) rows.load(a, p, w);
+    float c[4], s[4];
+    if (turn) load_phases<D>(a, p, c, s);
+    const char* others = in + (int64_t)head_of<NEAR>(p, w, 0) * share * plane;  // of a shared head
+    Raw8<BF16> more[3];
+    if (SHARED && share > 1) {
+      more[0].template load<true>(others + plane);
+      if (share > 2) {
+        more[1].template load<true>(others + 2 * plane);
+        more[2].template load<true>(others + min(3, share - 1) * plane);
+      }
+    }
+    loads_done();
+    if (NORM) rows.arrive(p);
+    char* out = static_cast<char*>(a.drows) + (p.t * a.stride + (int64_t)(w.first + p.slot) * D + 8 * sub) * kBytes;
+#pragma unroll
+    for (int i = 0; i < kBwdHeads; ++i) {
+      if (i << NEAR >= w.n) break;
+      const bool there = p.valid && p.slot + (i << NEAR) < w.n;
+      float u[8];
+      up[i].get(u);
+      if (SHARED && share > 1 && i == 0) {
+        float x[8];
+        for (int h = 1; h < share; h += 3) {
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            if (h + k >= share) break;
+            more[k].get(x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] += x[j];
+          }
+          if (h + 3 < share) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) more[k].template load<true>(others + min(h + 3 + k, share - 1) * plane);
+          }
+        }
+      }
+      if (turn) rotate<true>(u, c, s);
+      if (NORM) {
+        float x[8];
+        rows.under_norm(i, x);
+        const float r = rms_factor<D>(rows.squares(i), a.eps);
+        // with g' = r g, u' = w g': dw += g' x, dx = u' - x r^2 mean(u' x)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] *= r;
+        if (weight) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (there) dw[j] = fmaf(u[j], x[j], dw[j]);
+            u[j] *= wt[j];
+          }
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot = fmaf(u[j], x[j], dot);
+        dot = head_sum<kLanes>(dot) * (r * r * (1.f / D));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = fmaf(-x[j], dot, u[j]);
+      }
+      if (there) store8_stream<BF16>(out + (i << NEAR) * D * kBytes, u);
+    }
+    if (a.gate_dim == 1 && kind == kQ && w.h0 == 0)
+      move_logits<Bits<BF16>, true>(a, tile, (64 / kLanes) >> NEAR);
+  }
+}
+
+// Blocks [0, norm_blocks) take the heads of q and k and write a row of partial weight
+// gradients each, the others those of v and the gate.
 template <bool BF16, int D, bool CODES, bool SHARED, int NEAR>
 __global__ void __launch_bounds__(kWaves * 64) bwd_kernel(const QkvArgs a) {
-  constexpr int kLanes = D / 8, kBytes = BF16 ? 2 : 4;
+  constexpr int kLanes = D / 8;
   const int64_t block = block_index();
   const bool head = block < a.norm_blocks;
   const uint32_t in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -350,80 +440,10 @@ __global__ void __launch_bounds__(kWaves * 64) bwd_kernel(const QkvArgs a) {
   if (at_tile < a.stride_tiles) {
     const Work w = work_of<kBwdHeads, SHARED ? 1 : kBwdHeads, NEAR>(a, at_tile, group);
     kind = w.kind;
-    const bool turn = head && a.cs, norm = head && a.norm;
-    const float* weight = kind == kQ ? a.wq : a.wk;
-    float wt[8];
-    if (norm && weight) load_weights(weight, sub, wt);
-    const int64_t plane = a.per_tile * D * kBytes;
-    const int share = kind == kK || kind == kV ? a.share : 1;
-    const char* from = static_cast<const char*>(kind == kQ ? a.q : kind == kK ? a.k : kind == kV ? a.v : a.gate) +
-                       (int64_t)w.h0 * share * plane;
-    for (uint32_t tile = w.tile; tile < a.tiles; tile += a.stride_tiles) {
-      const Place p = place<D, NEAR>(a, tile);
-      const char* in = from + p.b * a.heads * plane + (p.r * D + 8 * sub) * kBytes;
-      Raw8<BF16> up[kBwdHeads];
-#pragma unroll
-      for (int i = 0; i < kBwdHeads; ++i) up[i].template load<true>(in + (int64_t)head_of<NEAR>(p, w, i) * share * plane);
-      const char* others = in + (int64_t)head_of<NEAR>(p, w, 0) * share * plane;  // of a shared head
-      Raw8<BF16> more[SHARED ? 3 : 1];
-      if (SHARED && share > 1) {
-#pragma unroll
-        for (int h = 1; h < 4; ++h) more[h - 1].template load<true>(others + min(h, share - 1) * plane);
-      }
-      Slices<BF16, D, CODES, kBwdHeads, NEAR, NEAR == 0> rows;
-      if (norm) rows.load(a, p, w);
-      float c[4], s[4];
-      if (turn) load_phases<D>(a, p, c, s);
-      loads_done();
-      if (norm) rows.arrive(p);
-      char* out = static_cast<char*>(a.drows) + (p.t * a.stride + (int64_t)(w.first + p.slot) * D + 8 * sub) * kBytes;
-#pragma unroll
-      for (int i = 0; i < kBwdHeads; ++i) {
-        if (i << NEAR >= w.n) break;
-        const bool there = p.valid && p.slot + (i << NEAR) < w.n;
-        float u[8];
-        up[i].get(u);
-        if (SHARED && share > 1 && i == 0) {
-          float x[8];
-          for (int h = 1; h < share; h += 3) {
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-              if (h + k >= share) break;
-              more[k].get(x);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] += x[j];
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) more[k].template load<true>(others + min(h + 3 + k, share - 1) * plane);
-          }
-        }
-        if (turn) rotate<true>(u, c, s);
-        if (norm) {
-          float x[8];
-          rows.under_norm(i, x);
-          const float r = rms_factor<D>(rows.squares(i), a.eps);
-          // with g' = r g, u' = w g': dw += g' x, dx = u' - x r^2 mean(u' x)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) u[j] *= r;
-          if (weight) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              if (there) dw[j] = fmaf(u[j], x[j], dw[j]);
-              u[j] *= wt[j];
-            }
-          }
-          float dot = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dot = fmaf(u[j], x[j], dot);
-          dot = head_sum<kLanes>(dot) * (r * r * (1.f / D));
-#pragma unroll
-          for (int j = 0; j < 8; ++j) u[j] = fmaf(-x[j], dot, u[j]);
-        }
-        if (there) store8_stream<BF16>(out + (i << NEAR) * D * kBytes, u);
-      }
-      if (a.gate_dim == 1 && kind == kQ && w.h0 == 0)
-        move_logits<Bits<BF16>, true>(a, tile, (64 / kLanes) >> NEAR);
-    }
+    if (head && a.norm)
+      backward<BF16, D, CODES, SHARED, NEAR, true>(a, w, dw);
+    else
+      backward<BF16, D, CODES, SHARED, NEAR, false>(a, w, dw);
   }
   if (!a.partial || !head) return;
   __shared__ float sums[kWaves][D];
@@ -532,7 +552,6 @@ static void plan(QkvArgs& a, int d, bool bf16, bool back) {
                   : ((int64_t)a.waves + kWaves - 1) / kWaves;
 }
 
-
 // Rows past the caches' replacement: where they are so many that none of them would be
 // found there again, and whole cache lines of them are read at a time (16 tiles of rows,
 // 4.3 GB: 1380 us so and 1410 otherwise; 0.27 GB: 89 and 83 us; off the lines 840 and 813).
@@ -593,8 +612,12 @@ static void run(const QkvArgs& a, int d, bool back, hipStream_t s) {
   if (d == 128) run_d<BF16, 128>(a, back, s);
 }
 
-// Rows that one block of the sum takes: a second launch adds up to 64 blocks' results.
-constexpr int kSumRows = 256;
+// Rows that one block of the first sum takes, of at most 2^15 blocks; a second launch adds theirs.
+static int sum_rows(const QkvArgs& a) {
+  const int64_t span = (a.norm_blocks + (1 << 15) - 1) >> 15;
+  return (int)(span < 256 ? 256 : span);
+}
+static int64_t sums_of(const QkvArgs& a) { return (a.norm_blocks + sum_rows(a) - 1) / sum_rows(a); }
 
 }  // namespace qkv
 
@@ -605,8 +628,7 @@ void launch_qkv_heads(QkvArgs a, int d, strata_dtype dt, hipStream_t s) {
 
 size_t qkv_bwd_partial_bytes(QkvArgs a, int d, strata_dtype dt) {
   qkv::plan(a, d, dt == STRATA_BF16, true);
-  const int64_t rows = a.norm_blocks, sums = (rows + qkv::kSumRows - 1) / qkv::kSumRows;
-  return (size_t)(rows + sums) * 2 * d * sizeof(float);
+  return (size_t)(a.norm_blocks + qkv::sums_of(a)) * 2 * d * sizeof(float);
 }
 
 void launch_qkv_heads_bwd(QkvArgs a, int d, strata_dtype dt, float* dwq, float* dwk, hipStream_t s) {
@@ -615,12 +637,12 @@ void launch_qkv_heads_bwd(QkvArgs a, int d, strata_dtype dt, float* dwq, float* 
   if (!a.partial) return;
   const float* in = a.partial;
   int64_t rows = a.norm_blocks;
-  if (rows > 2 * qkv::kSumRows) {
-    const int64_t sums = (rows + qkv::kSumRows - 1) / qkv::kSumRows;
+  if (qkv::sums_of(a) > 2) {
     float* out = a.partial + rows * 2 * d;
-    hipLaunchKernelGGL(qkv::weight_sum_kernel, dim3(2 * d / 32, (unsigned)sums), dim3(qkv::kSumThreads), 0, s, in, rows,
-                       qkv::kSumRows, 2 * d, out, nullptr, nullptr);
-    in = out, rows = sums;
+    const int span = qkv::sum_rows(a);
+    hipLaunchKernelGGL(qkv::weight_sum_kernel, dim3(2 * d / 32, (unsigned)qkv::sums_of(a)), dim3(qkv::kSumThreads), 0, s,
+                       in, rows, span, 2 * d, out, nullptr, nullptr);
+    in = out, rows = qkv::sums_of(a);
   }
   hipLaunchKernelGGL(qkv::weight_sum_kernel, dim3(2 * d / 32), dim3(qkv::kSumThreads), 0, s, in, rows, (int)rows, 2 * d,
                      nullptr, dwq, dwk);
