@@ -1,5 +1,7 @@
 """Projection rows into the head layout and back (strata_qkv_heads, _ckpt, _bwd)
 against the float64 oracle: types, head layouts, odd grids, one token, padding."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -7,7 +9,7 @@ import torch
 from oracle import rows as R
 from paper_2606_31248_amd import binding as B
 
-from _rows import Case, Problem, TYPE, check_grads, check_heads, f64, guarded, normal, gen
+from _rows import Case, Problem, TYPE, check_grads, check_heads, gen, normal, phases
 
 pytestmark = pytest.mark.gpu
 
@@ -26,6 +28,17 @@ CASES = [
     Case("bf16", 1, 4, 4, 2, 5, 5, 64, rope=False, norm=False, weights=False),   # layout alone
     Case("bf16", 2, 16, 16, 4, 16, 16, 64, gate=64),                      # many waves
     Case("bf16", 1, 3, 3, 24, 33, 31, 32, gate=1),
+    # rows off the cache lines with heads enough to lie beside each other in a wave of the backward
+    Case("bf16", 2, 16, 16, 2, 5, 7, 64, gate=64, pad=8),
+    Case("bf16", 1, 11, 11, 3, 5, 5, 64, gate=64, pad=16),                # 11 of 12 places taken
+    Case("bf16", 2, 16, 4, 3, 5, 3, 64, gate=1),
+    Case("bf16", 1, 16, 8, 2, 5, 9, 32, gate=32, pad=8),
+    Case("bf16", 3, 4, 2, 1, 7, 3, 128, gate=1, weights=False),
+    Case("f32", 1, 8, 4, 2, 5, 3, 64, gate=1),
+    # shared heads in several rounds of loads
+    Case("bf16", 1, 10, 2, 2, 3, 5, 64),
+    Case("bf16", 2, 16, 1, 1, 4, 9, 64, gate=1),
+    Case("f32", 1, 7, 1, 2, 3, 5, 32, gate=32),
 ]
 IDS = [f"{c.dtype}-{c.B}x{c.heads}.{c.kv}x{c.Z}x{c.H}x{c.W}x{c.d}-g{c.gate}p{c.pad}" for c in CASES]
 
@@ -87,6 +100,40 @@ def test_backward_from_eight_bits(c):
     assert torch.equal(got["drows"][..., :c.p.width], other["drows"][..., :c.p.width])
     for n in ("dwq", "dwk"):
         assert got[n] is None or torch.equal(got[n], other[n])
+
+
+def test_backward_of_many_tokens_with_one_head():
+    """70656 tokens of one 128-channel head: a wave takes several tiles, the weights' sums two launches."""
+    c = Case("bf16", 1, 1, 1, 24, 64, 46, 128, gate=0)
+    x = Problem(c, 11)
+    got = x.backward(x.rows)
+    x.check_guards()
+    want = x.want_backward(x.rows64())
+    # here the sums have up to 5 additions in a lane, 2 in a block and 50 in the two sums: within WEIGHT_SUM
+    check_grads(got, want, c.dtype, "backward")
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_many_tiles_equal_each_tile_alone(codes):
+    """Rows past 2^29 elements (and offsets past 2^32 bytes): the same bits as tile by tile."""
+    c = Case("bf16", 9, 16, 16, 8, 64, 64, 64, gate=64)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    rows = torch.empty(c.grid + (4096,), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    cs = phases(c, gen(13))
+    w = torch.linspace(0.5, 1.5, 64, device="cuda")
+
+    def run(b, r, table):
+        one = dataclasses.replace(c, B=b)
+        out = [torch.empty(one.shape, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+        kept = [torch.empty(one.grid + (4096,), dtype=torch.int8, device="cuda"),
+                torch.empty(one.grid + (128,), dtype=torch.uint8, device="cuda")] if codes else [None, None]
+        B.strata_qkv_heads(one.desc(), r, w, w, table, *out, *kept)
+        return out + [t for t in kept if t is not None]
+
+    whole = run(9, rows, cs)
+    for b in (0, 4, 8):
+        for got, want in zip(whole, run(1, rows[b:b + 1].contiguous(), cs[b:b + 1].contiguous())):
+            assert torch.equal(got[b:b + 1], want)
 
 
 def test_gradient_against_differences():
