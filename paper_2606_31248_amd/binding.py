@@ -582,7 +582,8 @@ def _ckpt_args(x, codes, scales):
         if not (type(t) is torch.Tensor and t.dtype is dt and t.device == dev and t.numel() == many
                 and t.is_contiguous()):
             _need(name, t, None, dt, dev)
-            raise ValueError(f"{name}: {t.numel()} elements, expected {many}")
+            if t.numel() != many:
+                raise ValueError(f"{name}: {t.numel()} elements, expected {many}")
     return n, x.data_ptr(), codes.data_ptr(), scales.data_ptr()
 
 

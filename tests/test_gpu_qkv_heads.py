@@ -39,6 +39,7 @@ CASES = [
     Case("bf16", 1, 10, 2, 2, 3, 5, 64),
     Case("bf16", 2, 16, 1, 1, 4, 9, 64, gate=1),
     Case("f32", 1, 7, 1, 2, 3, 5, 32, gate=32),
+    Case("bf16", 1, 70, 35, 1, 2, 3, 32, gate=1),                         # more logits a token than lanes
 ]
 IDS = [f"{c.dtype}-{c.B}x{c.heads}.{c.kv}x{c.Z}x{c.H}x{c.W}x{c.d}-g{c.gate}p{c.pad}" for c in CASES]
 
@@ -173,6 +174,44 @@ def test_extreme_rows(dtype):
     out, got = x.forward(), x.backward(x.rows)
     check_heads(out, x.want_forward(x.rows64()), dtype, "forward")
     check_grads(got, x.want_backward(x.rows64()), dtype, "backward")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_extreme_rows_in_eight_bits(dtype):
+    """Heads from 0 to the largest finite values, whose squares overflow or vanish, in 8 bits: heads made again and
+    gradients equal those of rows that hold the decoded values (with NaN where they have NaN)."""
+    c = Case(dtype, 1, 4, 2, 1, 2, 6, 64, gate=64)
+    x = Problem(c, 14)
+    x.rows = normal(tuple(x.rows.shape), dtype, gen(15)).clamp(-1.5, 1.5)
+    size = torch.tensor([0.0, 2.0 ** -126, 2.0 ** -100, 2.0 ** -63, 2.0 ** -20, 1.0, 2.0 ** 20, 2.0 ** 62, 2.0 ** 64, 2.0 ** 100,
+                         2.0 ** 125, 2.0 ** 127]).view(1, 1, 2, 6, 1)
+    x.rows *= size.to(TYPE[dtype]).cuda()
+    codes, scales = x.codes_out()
+    x.forward(codes, scales)
+    assert int(scales.max()) == 254 and int(scales.min()) == 7
+    again, got = x.again(codes, scales), x.backward(None, codes, scales)
+    held = torch.empty(c.grid + (c.p.kept,), dtype=TYPE[dtype], device="cuda")
+    B.strata_ckpt_unpack(codes, scales, held)
+    x.rows = held.contiguous()
+    other, want = x.forward(), x.backward(x.rows)
+    same = lambda a, b: bool(((a == b) | (a.isnan() & b.isnan())).all())  # noqa: E731
+    for n in other:
+        assert same(again[n], other[n]), n
+    for n in want:
+        assert same(got[n], want[n]), n
+
+
+def test_zero_heads_without_eps():
+    """eps = 0: a zero head has no norm (NaN), from rows and from 8 bits, and its neighbours keep theirs."""
+    c = Case("bf16", 1, 4, 4, 1, 2, 4, 64)
+    x = Problem(c, 16)
+    x.desc.eps = 0.0
+    x.rows[0, 0, 1, 2, 64:128] = 0
+    codes, scales = x.codes_out()
+    out, again = x.forward(codes, scales), x.again(codes, scales)
+    for o in (out, again):
+        bad = o["q"].isnan().any(-1)
+        assert int(bad.sum()) == 1 and bool(bad[0, 1, 0, 1, 2]) and not o["k"].isnan().any()
 
 
 def test_a_broken_row_stays_alone():
