@@ -78,6 +78,7 @@ struct Raw8<false> {
   }
 };
 
+// past the caches' replacement in bf16 (float32: its two halves meet in the caches)
 template <bool BF16>
 __device__ __forceinline__ void store8_stream(void* p, const float (&v)[8]) {
   if (BF16) {
