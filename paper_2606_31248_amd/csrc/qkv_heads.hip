@@ -512,17 +512,22 @@ static int mode_of(const QkvArgs& a) { return a.codes ? kFromCodes : a.out_codes
 // Waves, two rounds of the card's, that a backward keeps when a wave takes several tiles.
 constexpr int64_t kFill = 16384;
 
-static constexpr int near_of(int d) { return d == 32 ? 3 : d == 64 ? 2 : 1; }
+// Most neighbouring heads of a token that a wave holds beside each other (log2).  Training tile, rows 32 bytes off the
+// lines, microseconds with 0, 1, 2, 3 (head_dim 64): 16 heads 1600, 1330, 1290, 1230; 8 heads 807, 647, 660, 590;
+// 6 heads 509, 429; 4 heads 328, 267, 273; 2 heads 181, 152.  16 heads of 32 channels with 2, 3, 4: 680, 650, 770.
+static constexpr int most_near(int d) { return d == 128 ? 2 : 3; }
 
 static void plan(QkvArgs& a, int d, bool bf16, bool back) {
   const int nh = back ? kBwdHeads : fwd_heads(mode_of(a)), nk = back && a.heads > a.kv ? 1 : nh;
-  // The backward of rows that do not start on cache lines: neighbouring heads of a token beside each other in a wave,
-  // 512 bytes of a bf16 row at a time, unless a tenth of the lanes would have none.
+  // The backward of rows that do not start on cache lines: as many neighbouring heads of a token beside each other in
+  // a wave as leave less than a tenth of the lanes without one.
   a.near = 0;
   if (back && a.stride * (bf16 ? 2 : 4) % 128) {
-    const int step = 1 << near_of(d), up_h = (a.heads + step - 1) / step * step, up_kv = (a.kv + step - 1) / step * step;
-    const int gates = a.gate_dim > 1;
-    if (10LL * (up_h * (1 + gates) + 2LL * up_kv) <= 11LL * a.slices) a.near = near_of(d);
+    const int64_t gates = a.gate_dim > 1;
+    for (a.near = most_near(d); a.near > 0; --a.near) {
+      const int64_t step = 1 << a.near, up_h = (a.heads + step - 1) / step * step, up_kv = (a.kv + step - 1) / step * step;
+      if (10 * (up_h * (1 + gates) + 2 * up_kv) <= 11 * (int64_t)a.slices) break;
+    }
   }
   const int per = 512 / d >> a.near, ph = nh << a.near, pk = nk << a.near;
   a.groups_q = (a.heads + ph - 1) / ph, a.groups_k = (a.kv + pk - 1) / pk;
@@ -597,12 +602,13 @@ static void run_bwd(const QkvArgs& a, hipStream_t s) {
 
 template <bool BF16, int D>
 static void run_d(const QkvArgs& a, bool back, hipStream_t s) {
-  if (!back)
-    run_fwd<BF16, D>(a, s);
-  else if (a.near)
-    run_bwd<BF16, D, near_of(D)>(a, s);
-  else
-    run_bwd<BF16, D, 0>(a, s);
+  if (!back) return run_fwd<BF16, D>(a, s);
+  switch (a.near) {
+    case 0: return run_bwd<BF16, D, 0>(a, s);
+    case 1: return run_bwd<BF16, D, 1>(a, s);
+    case 2: return run_bwd<BF16, D, 2>(a, s);
+    default: return run_bwd<BF16, D, most_near(D)>(a, s);
+  }
 }
 
 template <bool BF16>

@@ -34,6 +34,10 @@ CASES = [
     Case("bf16", 2, 16, 4, 3, 5, 3, 64, gate=1),
     Case("bf16", 1, 16, 8, 2, 5, 9, 32, gate=32, pad=8),
     Case("bf16", 3, 4, 2, 1, 7, 3, 128, gate=1, weights=False),
+    Case("bf16", 1, 4, 4, 2, 5, 3, 128, gate=128, pad=8),
+    Case("bf16", 1, 16, 16, 1, 5, 3, 32, gate=32, pad=16),
+    Case("bf16", 2, 6, 6, 1, 3, 5, 64, gate=64, pad=8),
+    Case("bf16", 1, 2, 2, 3, 3, 3, 64, gate=1),
     Case("f32", 1, 8, 4, 2, 5, 3, 64, gate=1),
     # shared heads in several rounds of loads
     Case("bf16", 1, 10, 2, 2, 3, 5, 64),
