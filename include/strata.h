@@ -309,7 +309,7 @@ strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* c
  * least strata_qkv_heads_bwd_workspace_size(desc) bytes of device memory with
  * weights, else it may be NULL; calls in flight at once need one each.  Buffers must
  * not overlap.  Rows that start on 128-byte lines (row_stride a multiple of 64 in
- * bf16) are written fastest: others take about 1.4 times as long. */
+ * bf16) are written fastest: others take 1.2 to 1.5 times as long. */
 size_t strata_qkv_heads_bwd_workspace_size(const strata_qkv_desc* desc);
 strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows, const int8_t* codes,
                                    const uint8_t* scales, const float* wq, const float* wk, const float* cs,
