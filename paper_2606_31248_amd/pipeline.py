@@ -52,10 +52,18 @@ def na3d_forward(q, k, v, window, scale, cs=None, out=None, lse=None):
     return out
 
 
+# what the attention's lse and output depend on, of a BlockSaved
+_OF_THE_FORWARD = frozenset(("qkv", "window", "scale", "wq", "wk", "cs", "rows"))
+
+
 @dataclasses.dataclass
 class BlockSaved:
-    """What block_backward needs: the rows and the attention's output, each as it was or as
-    (codes, scales), the softmax's lse and, with a gate logit per head, the gate."""
+    """What a block keeps: the rows and the attention's output, each as it was or as (codes, scales), the
+    softmax's lse and, with a gate logit per head, the gate.
+
+    out and lse are the forward's.  `again`: they are not those of the values that block_backward works on (rows
+    in 8 bits, or a field that shapes the attention assigned since), and it runs the attention once more for its own;
+    out is then for the caller, whose projection behind the block takes its weights' gradient from it."""
     qkv: B.QKVDesc
     window: tuple
     scale: float
@@ -66,6 +74,12 @@ class BlockSaved:
     rows: object
     out: object
     gate: Optional[torch.Tensor] = None
+    again: bool = False
+
+    def __setattr__(self, name, value):
+        if name in _OF_THE_FORWARD and "again" in self.__dict__:  # the last field: not while it is being made
+            self.__dict__["again"] = True
+        super().__setattr__(name, value)
 
     def nbytes(self) -> int:
         """Bytes kept for this block, besides the weights and the phases that all blocks share."""
@@ -92,7 +106,8 @@ def block_forward(rows, qkv: B.QKVDesc, window, scale, wq=None, wk=None, cs=None
     """Attention of one block from its projection's rows [B, Z, H, W, row_stride]: (out, saved).
 
     out: [B, heads, Z, H, W, head_dim], gated by the rows' gate logits if there are any.  eight_bit: `saved`
-    holds the rows and out in 8 bits (just over half the bytes of bf16) instead of the tensors themselves."""
+    holds the rows and out in 8 bits (just over half the bytes of bf16) instead of the tensors themselves, and
+    block_backward runs the attention's forward once more."""
     q, k, v, gate = _heads_like(qkv, rows.dtype, rows.device)
     kept = rows
     codes = scales = None
@@ -112,14 +127,15 @@ def block_forward(rows, qkv: B.QKVDesc, window, scale, wq=None, wk=None, cs=None
                 torch.empty((out.numel() + 31) // 32, dtype=torch.uint8, device=out.device))
         B.strata_ckpt_pack(out, *held)
     return out, BlockSaved(qkv, tuple(window), scale, wq, wk, cs, lse, kept, held,
-                           gate if qkv.gate_dim == 1 else None)
+                           gate if qkv.gate_dim == 1 else None, again=eight_bit)
 
 
 def block_backward(saved: BlockSaved, dout):
     """Gradient of block_forward's out: (drows [B, Z, H, W, row_stride], dwq, dwk), zeros behind the rows' width.
 
-    From 8 bits the gradients are those of the attention at the values that the codes stand for, with the
-    lse of the values they were made from."""
+    From 8 bits they are the gradients at the values that the codes stand for: the attention's forward is run
+    again on these, since weights exp(s - lse) with the lse of the values before would not sum to 1 (and exceed the
+    range that the attention's backward has for them)."""
     d = saved.qkv
     q, k, v, gate = _heads_like(d, dout.dtype, dout.device)
     rows, codes, scales = (None, *saved.rows) if isinstance(saved.rows, tuple) else (saved.rows, None, None)
@@ -127,16 +143,17 @@ def block_backward(saved: BlockSaved, dout):
         B.strata_qkv_heads_ckpt(d, codes, scales, saved.wq, saved.wk, saved.cs, q, k, v,
                                 gate if d.gate_dim > 1 else None)
         gate = saved.gate if d.gate_dim == 1 else gate
-        out = torch.empty_like(dout)
-        B.strata_ckpt_unpack(*saved.out, out)
     else:
         B.strata_qkv_heads(d, rows, saved.wq, saved.wk, saved.cs, q, k, v, gate)
-        out = saved.out
     desc, opts = _attention_of(d, saved.window, saved.scale, gate)
+    out, lse = saved.out, saved.lse
+    if saved.again:
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+        B.strata_na3d_fwd_ex(desc, opts, q, k, v, None, out, lse)
     dq, dk, dv = (torch.empty_like(q) for _ in range(3))
     dgate = None if gate is None else torch.empty_like(gate)
     ws = torch.empty(B.strata_na3d_bwd_ex_workspace_size(desc, opts), dtype=torch.uint8, device=q.device)
-    B.strata_na3d_bwd_ex(desc, opts, q, k, v, None, out, dout, saved.lse, dq, dk, dv, dgate, ws)
+    B.strata_na3d_bwd_ex(desc, opts, q, k, v, None, out, dout, lse, dq, dk, dv, dgate, ws)
     drows = torch.empty((d.B, d.Z, d.H, d.W, d.row_stride), dtype=dout.dtype, device=dout.device)
     if d.row_stride > d.width:
         drows[..., d.width:] = 0

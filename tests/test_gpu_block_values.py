@@ -1,0 +1,98 @@
+"""The block's gradient where the softmax is peaked (norm scales of 4, or no norm and rows of standard deviation 4:
+logits of deviation 16): from 8 bits it is the gradient of the block at the values that the codes stand for, whose
+softmax is their own."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import rows as R
+from paper_2606_31248_amd import binding as B
+from paper_2606_31248_amd import pipeline
+
+from _rows import TYPE, Case, Problem, f64, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    (Case("bf16", 1, 2, 1, 5, 13, 11, 64, gate=64), (5, 9, 9)),
+    (Case("bf16", 1, 2, 2, 9, 9, 11, 64, gate=1, pad=8), (9, 9, 9)),
+    (Case("bf16", 2, 4, 2, 8, 12, 10, 64), (3, 7, 7)),
+    (Case("bf16", 1, 2, 1, 6, 5, 5, 64, rope=False), (6, 1, 1)),
+    (Case("bf16", 1, 1, 1, 9, 9, 10, 128, gate=128), (9, 9, 9)),
+    (Case("f32", 1, 2, 1, 3, 7, 9, 32, gate=1), (3, 5, 7)),
+    (Case("bf16", 2, 2, 1, 8, 12, 10, 64, gate=64, norm=False, weights=False), (3, 7, 7)),
+    (Case("bf16", 1, 2, 2, 5, 11, 9, 64, norm=False, weights=False), (5, 9, 9)),
+    (Case("f32", 1, 2, 1, 3, 7, 9, 64, norm=False, weights=False), (3, 5, 7)),
+]
+
+# Relative to the whole array.  bf16: the library's 2e-2 for logits of order one, and 2^-11 sqrt(2/3) (the float16 copies of
+# q and k, uniform) of logits of deviation 16 in the logit and in its lse, 1.3e-2.  float32: scale sum |q_e k_e| is about 82
+# here, with up to 8 roundings of 2^-24 in a logit and in its lse 8e-5 of a weight, and half as much in the sums.
+LIMIT = {"bf16": 3.3e-2, "f32": 1.2e-4}
+
+
+def peaked(c, seed):
+    x = Problem(c, seed)
+    x.rows = normal(tuple(x.rows.shape), c.dtype, gen(seed + 100), 1.0 if c.norm else 4.0)
+    if c.weights:
+        x.wq, x.wk = 4 * x.wq, 4 * x.wk
+    return x
+
+
+def exact_grads(c, window, x, dout):
+    """float64 gradients at x.rows of the attention on the heads that the library makes of them, whose output it
+    stores in its own type: with d = <dout, exact - stored> that output moves dq by scale d_i sum_j P_ij k_j (the
+    forward on v = k) and dk by scale sum_i P_ij d_i q_i (dv for dout = d q)."""
+    heads = {n: t for n, t in x.forward().items() if t is not None}
+    desc, opts = pipeline._attention_of(x.desc, window, c.d ** -0.5, heads.get("gate"))
+    stored = torch.empty_like(heads["q"])
+    B.strata_na3d_fwd_ex(desc, opts, heads["q"], heads["k"], heads["v"], None, stored, None)
+    q, k, v = (f64(heads[n]) for n in "qkv")
+    gate, scale, up = f64(heads.get("gate")), c.d ** -0.5, f64(dout)
+    exact = oracle.na3d_fwd(q, k, v, window, scale, gate=gate)[0]
+    dq, dk, dv, *dgate = oracle.na3d_bwd(q, k, v, up, window, scale, gate=gate)
+    d = ((exact - f64(stored)) * up).sum(-1, keepdims=True)
+    dq = dq + scale * d * oracle.na3d_fwd(q, k, k, window, scale)[0]
+    dk = dk + scale * oracle.na3d_bwd(q, k, v, d * q, window, scale)[2]
+    return R.backward(c.p, x.rows64(), dq, dk, dv, dgate[0] if dgate else None, f64(x.wq), f64(x.wk), f64(x.cs))
+
+
+def check(c, got, want, what):
+    drows, dwq, dwk = got
+    a, b = c.heads * c.d, c.kv * c.d
+    parts = [(n, f64(drows)[..., lo:hi], want["drows"][..., lo:hi]) for n, lo, hi in (
+        ("q", 0, a), ("k", a, a + b), ("v", a + b, a + 2 * b), ("gate", a + 2 * b, c.p.width)) if hi > lo]
+    parts += [(n, f64(t), want[n]) for n, t in (("dwq", dwq), ("dwk", dwk)) if t is not None]
+    for n, g, w in parts:
+        err = np.linalg.norm(g - w) / np.linalg.norm(w)
+        print(f"{what} {n}: {err:.2e}")
+        assert err <= LIMIT[c.dtype], f"{what}: {n} off by {err:.2e}"     # NaN fails too
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("c,window", CASES)
+def test_gradient_at_the_kept_values(c, window, eight):
+    x = peaked(c, 1)
+    dout = normal(c.shape, c.dtype, gen(70))
+    _, saved = pipeline.block_forward(x.rows, x.desc, window, c.d ** -0.5, x.wq, x.wk, x.cs, eight_bit=eight)
+    got = pipeline.block_backward(saved, dout)
+    if eight:
+        held = torch.empty(c.grid + (c.p.kept,), dtype=TYPE[c.dtype], device="cuda")
+        B.strata_ckpt_unpack(*saved.rows, held)
+        x.rows[..., :c.p.kept] = held
+    check(c, got, exact_grads(c, window, x, dout), "8 bits" if eight else "rows")
+
+
+def test_other_rows_than_the_forward_read():
+    """Rows or weights assigned between forward and backward: the gradient of the block on them, bit for bit."""
+    c, window = CASES[0]
+    x = peaked(c, 2)
+    dout = normal(c.shape, c.dtype, gen(71))
+    forward = lambda rows, w: pipeline.block_forward(rows, x.desc, window, c.d ** -0.5, w, x.wk, x.cs)[1]  # noqa: E731
+    rows, w = normal(tuple(x.rows.shape), c.dtype, gen(72)), 0.5 * x.wq
+    want = pipeline.block_backward(forward(rows, w), dout)
+    saved = forward(x.rows, x.wq)
+    saved.rows, saved.wq = rows, w
+    for g, h in zip(pipeline.block_backward(saved, dout), want):
+        assert torch.equal(g, h)
