@@ -171,7 +171,6 @@ struct Slices {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= f;
   }
-  __device__ __forceinline__ void under_norm(int i, float (&v)[8]) const { raw[i].get(v); }
 };
 
 // Codes.  Of two of its slices an even lane loads its own and the next lane's 8 codes
@@ -210,7 +209,6 @@ struct Slices<BF16, D, true, NH, NEAR, STREAM> {
   __device__ __forceinline__ void scaled(int i, float f, float (&v)[8]) const {
     decode8_times(code[i], norm_step(i), f, v);
   }
-  __device__ __forceinline__ void under_norm(int i, float (&v)[8]) const { decode8_times(code[i], norm_step(i), 1.f, v); }
   __device__ __forceinline__ float norm_step(int i) const { return e[i] == 254 ? 0.f : step_of(e[i]); }
 };
 
@@ -396,25 +394,26 @@ __device__ __forceinline__ void backward(const QkvArgs& a, const Work& w, float 
       }
       if (turn) rotate<true>(u, c, s);
       if (NORM) {
-        float x[8];
-        rows.under_norm(i, x);
+        float y[8];
         const float r = rms_factor<D>(rows.squares(i), a.eps);
-        // with g' = r g, u' = w g': dw += g' x, dx = u' - x r^2 mean(u' x)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] *= r;
+        rows.scaled(i, r, y);
+        // with y = r x, u' = r w g: dw += g y, dx = u' - y mean(u' y), r never squared: it may reach 2^74
         if (weight) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            if (there) dw[j] = fmaf(u[j], x[j], dw[j]);
+            if (there) dw[j] = fmaf(u[j], y[j], dw[j]);
             u[j] *= wt[j];
           }
         }
         float dot = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dot = fmaf(u[j], x[j], dot);
-        dot = head_sum<kLanes>(dot) * (r * r * (1.f / D));
+        for (int j = 0; j < 8; ++j) {
+          u[j] *= r;
+          dot = fmaf(u[j], y[j], dot);
+        }
+        dot = head_sum<kLanes>(dot) * (1.f / D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = fmaf(-x[j], dot, u[j]);
+        for (int j = 0; j < 8; ++j) u[j] = fmaf(-y[j], dot, u[j]);
       }
       if (there) store8_stream<BF16>(out + (i << NEAR) * D * kBytes, u);
     }
