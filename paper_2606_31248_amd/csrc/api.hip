@@ -339,7 +339,7 @@ static strata_status check_qkv(const strata_qkv_desc* d, bool with_rows, QkvArgs
   a->tokens = tokens;
   a->per_tile = zh * d->W;
   a->hw = (int64_t)d->H * d->W;
-  a->stride = d->row_stride;
+  a->stride = with_rows ? d->row_stride : 0;
   a->kept = kept;
   a->heads = d->heads;
   a->kv = d->kv_heads;
