@@ -265,7 +265,10 @@ strata_status strata_na3d_bwd_ex(const strata_na3d_desc* desc, const strata_na3d
  * NULL: the identity).  The attention is then called with cs == NULL and without
  * its own norm.  w_q, w_k: float32 [d] on the device, the learned scale of the norm
  * shared by all heads, both or neither (NULL: 1); they need qk_norm.  Arithmetic in
- * float32, one rounding to dtype. */
+ * float32, one rounding to dtype.  Range of the norm, here and in the two calls below:
+ * a head of root mean square 2^64 / sqrt(d) and more has squares that overflow, and a
+ * norm and a gradient of 0; with eps below 2^-126 a mean square below 2^-126 keeps
+ * fewer digits (17 bits at a root of 2^-66) and one of 0 makes the head NaN. */
 typedef struct {
   int32_t B, heads, kv_heads, Z, H, W, head_dim; /* kv_heads divides heads */
   int32_t gate_dim;   /* gate logits per head in the rows: 0 (none), 1 or head_dim */
@@ -288,8 +291,10 @@ strata_status strata_qkv_heads(const strata_qkv_desc* desc, const void* rows, co
                                uint8_t* scales, void* stream);
 
 /* The same from the 8-bit form: equal bit for bit to strata_qkv_heads on rows that
- * hold the values of the codes (where a head's sum of squares overflows and its norm
- * is 0, but for the sign of that 0).  row_stride is not used; gate must be NULL when
+ * hold the values of the codes, as long as the norm stays among float32's normal
+ * numbers: not for the sign of the 0 of a head whose squares overflow, for squares
+ * below 2^-126 beside an eps as small, or for normalised elements below 2^-126.
+ * row_stride is not used; gate must be NULL when
  * gate_dim == 1. */
 strata_status strata_qkv_heads_ckpt(const strata_qkv_desc* desc, const int8_t* codes, const uint8_t* scales,
                                     const float* wq, const float* wk, const float* cs, void* q, void* k, void* v,
@@ -321,9 +326,10 @@ strata_status strata_qkv_heads_bwd(const strata_qkv_desc* desc, const void* rows
  * scales[g] = s, a biased exponent, and codes[i] with the value codes[i] * 2^(s - 133).
  * With A the group's largest magnitude, 2^(s - 133) is the smallest power of two for
  * which A rounds to at most 127 steps, and at least 2^-126 (s >= 7); codes are
- * rounded to nearest, ties to even: the error of an element is at most half a step,
- * A/127, and the rms error of normal data about 0.9 % of its standard deviation.
- * At s = 254 (A >= 1.992 * 2^127) codes are clamped to +-127.  A group with an
+ * rounded to nearest, ties to even: the error of an element is at most half a step.
+ * For 7 < s < 254 that is at most A/127, and the rms error of normal data about 0.9 %
+ * of its standard deviation.  At s = 7 it is 2^-127, whatever A; at s = 254, where
+ * codes are clamped to +-127 (A >= 1.992 * 2^127), less than one step.  A group with an
  * infinity or a NaN has s = 255 and codes 0 and stands for 32 NaN.  Encoding is
  * exact arithmetic; decoded values are exact in bf16 (7 bits).
  * x: [n] of dtype; codes: int8 [n]; scales: uint8 [ceil(n / 32)]; 1 <= n < 2^40. */

@@ -157,7 +157,8 @@ __device__ __forceinline__ void decode8(uint2 c, float step, float (&v)[8]) {
 }
 
 // 8 codes -> values times f, rounded once: (code + 128) F - 128 F with F = step f.
-// F has to stay below 2^120: a step of 2^121 only with f = 0.
+// F has to stay below 2^120 (a step of 2^121 only with f = 0); as a subnormal it is
+// itself rounded.
 __device__ __forceinline__ void decode8_times(uint2 c, float step, float f, float (&v)[8]) {
   const uint2 w = flip(c);
   const float m = step * f, off = -128.f * m;
@@ -166,7 +167,7 @@ __device__ __forceinline__ void decode8_times(uint2 c, float step, float f, floa
 }
 
 // Sum of the squares of 8 codes, below 2^17 and so exact, as the sum of their values'
-// squares over step^2 is in float32
+// squares over step^2 is in float32 where those are normal numbers
 __device__ __forceinline__ float code_squares(uint2 c) {
   return (float)__builtin_amdgcn_sdot4((int)c.x, (int)c.x, __builtin_amdgcn_sdot4((int)c.y, (int)c.y, 0, false), false);
 }

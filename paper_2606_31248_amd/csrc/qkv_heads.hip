@@ -175,7 +175,8 @@ struct Slices {
 
 // Codes.  Of two of its slices an even lane loads its own and the next lane's 8 codes
 // of the first, an odd lane the same of the second; a swap gives each lane its 8 of
-// both.  Steps are powers of two, so that each result equals the rows' bit for bit.
+// both.  Steps are powers of two, so that each result equals the rows' bit for bit while
+// squares and normalised values stay normal numbers (below, each path rounds its own way).
 // A step of 2^121 makes a sum of squares infinite and the factor 0: the norm's values
 // are then 0 whatever the codes, and their step is taken as 0.
 template <bool BF16, int D, int NH, int NEAR, bool STREAM>
