@@ -329,7 +329,8 @@ static strata_status check_qkv(const strata_qkv_desc* d, bool with_rows, QkvArgs
   REQUIRE(!with_rows || (d->row_stride >= width && d->row_stride % 8 == 0),
           "qkv desc: row_stride %lld must be a multiple of 8 and at least the row's %lld elements",
           (long long)d->row_stride, (long long)width);
-  // a launch takes 2^24 blocks of 16 tokens (head_dim 128); rows and heads of that many exceed a card
+  // FastDiv divides token and wave numbers below 2^31: a wave takes at least 512 elements of a row's heads (or one
+  // head's of a last, shorter tile), so that as many waves would be 2^40 elements, more than a card holds
   const int64_t most = (int64_t)1 << 28, zh = (int64_t)d->Z * d->H;
   REQUIRE(zh < most && zh * d->W < most && zh * d->W * d->B < most, "qkv desc: 2^28 tokens or more");
   const int64_t tokens = zh * d->W * d->B;

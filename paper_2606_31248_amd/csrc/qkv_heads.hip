@@ -181,6 +181,7 @@ struct Slices {
 // are then 0 whatever the codes, and their step is taken as 0.
 template <bool BF16, int D, int NH, int NEAR, bool STREAM>
 struct Slices<BF16, D, true, NH, NEAR, STREAM> {
+  static_assert(NH % 2 == 0, "slices are loaded two at a time");
   uint2 code[NH];
   uint8_t e[NH];
   __device__ __forceinline__ void load(const QkvArgs& a, const Place& p, const Work& w) {
@@ -188,10 +189,6 @@ struct Slices<BF16, D, true, NH, NEAR, STREAM> {
     const int odd = p.sub & 1;
 #pragma unroll
     for (int i = 0; i < NH; ++i) e[i] = a.scales[(at + head_of<NEAR>(p, w, i) * D + 8 * p.sub) >> 5];
-    if (NH == 1) {
-      code[0] = *reinterpret_cast<const uint2*>(a.codes + at + head_of<NEAR>(p, w, 0) * D + 8 * p.sub);
-      return;
-    }
 #pragma unroll
     for (int i = 0; i + 1 < NH; i += 2) {  // of a last one without a second both lanes load the first, 16 codes each
       const u32x4 c = load16(a.codes + at + head_of<NEAR>(p, w, i + odd) * D + 8 * (p.sub - odd));
