@@ -512,6 +512,9 @@ constexpr int64_t kFill = 16384;
 // Most neighbouring heads of a token that a wave holds beside each other (log2).  Training tile, rows 32 bytes off the
 // lines, microseconds with 0, 1, 2, 3 (head_dim 64): 16 heads 1600, 1330, 1290, 1230; 8 heads 807, 647, 660, 590;
 // 6 heads 509, 429; 4 heads 328, 267, 273; 2 heads 181, 152.  16 heads of 32 channels with 2, 3, 4: 680, 650, 770.
+// In float32 a head is twice the lines, and gains less (rows 32 bytes off, with 0, 1, 2, 3): 16 heads, 4 tiles 1143, 1078,
+// 1101, 1085; 8 tiles of 8 heads 1400, 1358, 1304, 1256; 4 heads 706, 704, 704; 2 heads 317, 320; 16 heads of 32
+// channels 1352, 1271, 1234, 1231; 8 heads of 128 channels, 4 tiles 1213, 1180, 1168.
 static constexpr int most_near(int d) { return d == 128 ? 2 : 3; }
 
 static void plan(QkvArgs& a, int d, bool bf16, bool back) {

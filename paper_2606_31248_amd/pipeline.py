@@ -107,7 +107,8 @@ def block_forward(rows, qkv: B.QKVDesc, window, scale, wq=None, wk=None, cs=None
 
     out: [B, heads, Z, H, W, head_dim], gated by the rows' gate logits if there are any.  eight_bit: `saved`
     holds the rows and out in 8 bits (just over half the bytes of bf16) instead of the tensors themselves, and
-    block_backward runs the attention's forward once more."""
+    block_backward runs the attention's forward once more.  Its gradient is then off by about 2 % at logits of
+    order one and by more as they grow (13 % at a deviation of 16)."""
     q, k, v, gate = _heads_like(qkv, rows.dtype, rows.device)
     kept = rows
     codes = scales = None

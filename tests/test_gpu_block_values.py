@@ -96,3 +96,13 @@ def test_other_rows_than_the_forward_read():
     saved.rows, saved.wq = rows, w
     for g, h in zip(pipeline.block_backward(saved, dout), want):
         assert torch.equal(g, h)
+
+
+@pytest.mark.parametrize("c,window", [CASES[0], CASES[2], CASES[4]])
+def test_weights_near_one_stay_finite(c, window):
+    """Norm scales of 8 (logits of deviation 64): weights of the first forward's lse would exceed float16's range."""
+    x = peaked(c, 3)
+    x.wq, x.wk = 2 * x.wq, 2 * x.wk
+    _, saved = pipeline.block_forward(x.rows, x.desc, window, c.d ** -0.5, x.wq, x.wk, x.cs, eight_bit=True)
+    for t in pipeline.block_backward(saved, normal(c.shape, c.dtype, gen(73))):
+        assert bool(t.isfinite().all())
