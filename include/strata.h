@@ -154,6 +154,8 @@ strata_status strata_na3d_fwd(const strata_na3d_desc* desc, const void* q, const
  *   P_ij = exp(s_ij - lse_i),   D_i = <dout_i, out_i>,
  *   dv_j = sum_{i: j in N(i)} P_ij dout_i,    dS_ij = P_ij (<dout_i, v_j> - D_i),
  *   dq_i = R_i^T scale sum_j dS_ij R_j k_j,    dk_j = R_j^T scale sum_i dS_ij R_i q_i.
+ * lse and out have to be those of these q, k and v: with others P is no softmax, and
+ * weights above 2 leave the range of the float16 products (results may be infinite).
  * Deterministic (the one atomic operation is an integer maximum, whose result
  * does not depend on order).  workspace: device memory of at least
  * strata_na3d_bwd_workspace_size(desc) bytes (holds D, one word per (batch,

@@ -63,7 +63,8 @@ class BlockSaved:
 
     out and lse are the forward's.  `again`: they are not those of the values that block_backward works on (rows
     in 8 bits, or a field that shapes the attention assigned since), and it runs the attention once more for its own;
-    out is then for the caller, whose projection behind the block takes its weights' gradient from it."""
+    out is then for the caller, whose projection behind the block takes its weights' gradient from it.  A state that
+    the caller constructs (dataclasses.replace does) is taken to hold the lse and out of its rows unless it says again."""
     qkv: B.QKVDesc
     window: tuple
     scale: float
