@@ -1,0 +1,516 @@
+"""The operators that enter a training block and that use up its gradients, as cases that can be timed and checked.
+
+The residual stream's addition with its RMS norm (a learned scale for all tokens, or a
+gate, a scale and a shift for every tile, as conditioned blocks have them), its output
+in the type or in 8 bits, and the gradients; the norm of all gradients with the clip
+factor; AdamW over many tensors with its states in 32 bits or in 8.  Plain forms in
+elementary float32 operations, results in 64 bits, and the library's calls (`own`).
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+EPS = 1e-6                                              # under the norm's root
+LR, BETA1, BETA2, ADAM_EPS, DECAY = 2e-4, 0.9, 0.999, 1e-8, 1e-5
+STEP = 1000                                             # steps that the optimiser has behind it
+GROUP = 32                                              # elements that share an exponent in 8 bits
+M_UNIT, V_UNIT = 17, 33                                 # octaves from the exponent of a group's largest to one unit
+
+
+def _norm(name, kind, dtype, groups, group_rows, width, residual=True, gate=False, scale=True, shift=False, eight=False):
+    c = dict(kind=kind, dtype=dtype, groups=groups, group_rows=group_rows, width=width, residual=residual,
+             gate=gate and residual, scale=scale, shift=shift, eight=eight and width % GROUP == 0)
+    return dict(c, name=name) if name else c
+
+
+def _weights(name, kind, grads, blocks=0, width=0, count=0, most=0, shape=0, eight=False, copy=False, clip=False):
+    c = dict(kind=kind, grads=grads, blocks=blocks, width=width, count=count, most=most, shape=shape, eight=eight,
+             copy=copy, clip=clip)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # inference on one small float32 tile of 4 levels x 16 x 16 tokens: the smallest call, latency
+        _norm("norm_tiny_f32", "norm", "f32", 1, 1024, 128),
+        # a rollout step's tiles: 16 tiles of 8 x 64 x 64 tokens, 16 heads of 64 channels
+        _norm("norm_rollout", "norm", "bf16", 1, 16 * 8 * 64 * 64, 1024),
+        # the training tile: the norm's output in 8 bits, as a projection keeps it for its weights' gradient, and back
+        _norm("norm_train_8bit", "norm", "bf16", 1, 8 * 8 * 64 * 64, 1024, eight=True),
+        # the training tile forward and backward, a learned scale
+        _norm("norm_step_train", "step", "bf16", 1, 8 * 8 * 64 * 64, 1024),
+        # the decoder's full-resolution blocks: 128 channels, conditioned (a gate, scale and shift for every tile)
+        _norm("norm_step_decoder", "step", "bf16", 8, 24 * 64 * 64, 128, gate=True, shift=True),
+        # a float32 training step on a ragged grid with a width that is no multiple of anything (gradient checks)
+        _norm("norm_step_ragged_f32", "step", "f32", 4, 7 * 21 * 27, 203, gate=True, shift=True),
+        # rows as wide as a projection's inner layer, few of them
+        _norm("norm_step_wide", "step", "bf16", 1, 24 * 16 * 16, 8192, residual=False),
+        # the scales of one block's QK norm and a few vectors: the smallest step, latency
+        _weights("adamw_tiny", "adamw", "f32", count=4, most=128, shape=1),
+        # all weights of 24 blocks of 1024 channels, states in 32 bits, a copy in bf16 for the model
+        _weights("adamw_model", "adamw", "bf16", blocks=24, width=1024, copy=True),
+        # the same with the states in 8 bits, and their values as a checkpoint takes them
+        _weights("adamw_model_8bit", "adamw", "bf16", blocks=24, width=1024, eight=True, copy=True),
+        # the norm of those gradients and the factor that clips them
+        _weights("grad_norm_model", "gnorm", "bf16", blocks=24, width=1024),
+        # a whole update of a small model of 300 tensors of odd sizes: norm, clipping, AdamW with 8-bit states
+        _weights("update_odd_8bit", "adamw", "f32", count=300, most=200000, shape=2, eight=True, clip=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the same ranges: 1 token and 1 weight to the largest above, odd sizes, all types and forms."""
+    if rng.random() < 0.5:
+        kind, dtype = rng.choice(["norm", "step", "step"]), rng.choice(["bf16", "bf16", "bf16", "f32"])
+        width = _log(rng, 1, 8192) if rng.random() < 0.4 else rng.choice([32, 64, 128]) * rng.randint(1, 16)
+        most = (1 << (28 if dtype == "bf16" else 26)) // width
+        groups = rng.choice([1, 1, _log(rng, 1, 64)])
+        rows = _log(rng, 1, max(1, most // groups))
+        return _norm("", kind, dtype, groups, rows, width, residual=rng.random() < 0.8, gate=rng.random() < 0.5,
+                     scale=rng.random() < 0.8, shift=rng.random() < 0.4, eight=kind == "norm" and rng.random() < 0.5)
+    kind, grads = rng.choice(["adamw", "adamw", "gnorm"]), rng.choice(["bf16", "f32"])
+    eight, copy, clip = rng.random() < 0.5, rng.random() < 0.5, rng.random() < 0.5
+    if rng.random() < 0.4:
+        return _weights("", kind, grads, blocks=rng.randint(1, 12), width=64 * rng.randint(1, 16), eight=eight, copy=copy,
+                        clip=clip)
+    count = _log(rng, 1, 400)
+    return _weights("", kind, grads, count=count, most=_log(rng, 2, (1 << 28) // count), shape=rng.randint(3, 1 << 30),
+                    eight=eight, copy=copy, clip=clip)
+
+
+# ---- sizes ------------------------------------------------------------------------
+
+def _sizes(c):
+    """Elements of each tensor."""
+    if c["blocks"]:  # projection into q, k, v and gate, the one behind the attention, two of 4 times the width, norms
+        w = c["width"]
+        return [4 * w * w, w * w, 4 * w * w, 4 * w * w, w, w, 64, 64] * c["blocks"]
+    rng = random.Random(c["shape"])
+    return [_log(rng, 1, c["most"]) for _ in range(c["count"])]
+
+
+def _places(sizes):
+    """First element of each tensor among all states, in whole groups of 32, and the end."""
+    at = [0]
+    for n in sizes:
+        at.append(at[-1] + -(-n // GROUP) * GROUP)
+    return at
+
+
+def _type(name):
+    return torch.float32 if name == "f32" else torch.bfloat16
+
+
+# ---- inputs -----------------------------------------------------------------------
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _randn(g, shape, dtype=torch.float32, mult=1.0):
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(0.0, mult, generator=g)
+
+
+def _prepare_norm(c, g):
+    t, w = _type(c["dtype"]), c["width"]
+    rows = (c["groups"] * c["group_rows"], w)
+    s = dict(c=c, x=None, gate=None, scale=None, shift=None, dx=None, dgate=None, dscale=None, dshift=None)
+    s["res"] = _randn(g, rows, t, 2.0)
+    s["res"].mul_(torch.exp(0.5 * _randn(g, w)).to(t))   # channels differ in size
+    s["sum"] = torch.empty_like(s["res"]) if c["residual"] else None
+    if c["residual"]:
+        s["x"] = _randn(g, rows, t)
+    vector = lambda mean, dev: mean + dev * _randn(g, (c["groups"], w))  # noqa: E731
+    if c["gate"]:
+        s["gate"] = vector(0.5, 0.2)
+    if c["scale"]:
+        s["scale"] = vector(1.0, 0.2)
+    if c["shift"]:
+        s["shift"] = vector(0.0, 0.2)
+    if c["eight"]:
+        s["codes"] = torch.empty(rows, dtype=torch.int8, device="cuda")
+        s["scales"] = torch.empty((rows[0], w // GROUP), dtype=torch.uint8, device="cuda")
+        s["back"] = torch.empty(rows, dtype=torch.bfloat16, device="cuda")
+    else:
+        s["y"] = torch.empty(rows, dtype=t, device="cuda")
+    if c["kind"] == "step":
+        s["dy"], s["dsum"] = _randn(g, rows, t), _randn(g, rows, t)
+        s["dres"] = torch.empty_like(s["res"])
+        s["dx"] = torch.empty_like(s["res"]) if c["gate"] else None
+        for n in ("gate", "scale", "shift"):
+            if s[n] is not None:
+                s["d" + n] = torch.empty_like(s[n])
+    return s
+
+
+def _prepare_weights(c, g):
+    sizes = _sizes(c)
+    at = _places(sizes)
+    n, t = at[-1], _type(c["grads"])
+    behind = [i for k, size in enumerate(sizes) for i in range(at[k] + size, at[k + 1])]
+    behind = torch.tensor(behind, dtype=torch.int64, device="cuda")
+    s = dict(c=c, step=STEP, factor=None, norm=None, copy=None)
+    size = torch.exp(_randn(g, n // GROUP)).mul_(1e-3).repeat_interleave(GROUP)  # the gradients' sizes differ
+    s["p"] = _randn(g, n, mult=0.02)
+    s["g"] = _randn(g, n).mul_(size).to(t)
+    v = size.square_().mul_(torch.rand(n, device="cuda", generator=g).add_(0.5))
+    m = _randn(g, n, mult=0.25).mul_(v.sqrt())
+    for x in (s["p"], s["g"], m, v):
+        x[behind] = 0
+    if c["eight"]:
+        s["m"], s["m_scales"] = _encode(m, torch.full_like(m, 0.5), M_UNIT)
+        s["v"], s["v_scales"] = _encode(v, torch.full_like(v, 0.5), V_UNIT)
+        for n in ("m", "v"):
+            s[n + "_values"] = torch.empty(s[n].shape, dtype=torch.bfloat16, device="cuda")
+    else:
+        s["m"], s["v"], s["m_scales"], s["v_scales"] = m, v, None, None
+    if c["copy"]:
+        s["copy"] = s["p"].to(torch.bfloat16)
+    if c["clip"] or c["kind"] == "gnorm":
+        s["norm"] = torch.empty(2, device="cuda")
+        s["most"] = 0.5 * float(s["g"].double().square().sum().sqrt())
+    if own:  # what a training program keeps: the list of its tensors
+        from paper_2606_31248_amd import binding as B
+        cut = lambda x: [x[a:a + k] for a, k in zip(at, sizes)]  # noqa: E731
+        s["list"] = B.make_params(cut(s["p"]), cut(s["g"]), cut(s["copy"]) if c["copy"] else None)
+    return s
+
+
+def prepare(case, seed):
+    return (_prepare_norm if case["kind"] in ("norm", "step") else _prepare_weights)(case, _gen(seed))
+
+
+# ---- the plain forms ----------------------------------------------------------------
+
+def _exponent(bits):
+    """The exponent of a group, from its largest element's bits: one more where rounding to 4 bits would carry."""
+    return ((bits + 0x100000) >> 23).clamp(max=254)
+
+
+def _encode(x, random, unit):
+    """float32 values and numbers in [0, 1) that decide their rounding -> codes and exponents of groups of 32.
+    A group's unit lies `unit` octaves below its largest's exponent; 3 bits behind the leading one, signed for M_UNIT."""
+    e = _exponent(x.abs().view(-1, GROUP).amax(1).view(torch.int32))
+    up = ((127 + unit + 127 - e).clamp(1, 254) << 23).view(torch.float32)
+    t = (x.abs().view(-1, GROUP) * up[:, None]).view(-1)
+    ex = ((t.view(torch.int32) >> 23) - 127).clamp(min=3)
+    part = torch.floor(t * ((130 - ex) << 23).view(torch.float32) + random).to(torch.int32)
+    code = (ex - 3) * 8 + part
+    if unit == M_UNIT:
+        code += torch.where(x < 0, 128, 0).to(torch.int32)
+    else:
+        code = torch.where(x > 0, code.clamp(min=1), code)
+    return code.to(torch.uint8), e.to(torch.uint8)
+
+
+def _decode(codes, scales, unit):
+    c, e = codes.to(torch.int32), scales.to(torch.int32)
+    sign = torch.ones_like(c)
+    if unit == M_UNIT:
+        sign = 1 - 2 * (c >> 7)
+        c = c & 127
+    whole = torch.where(c < 8, c, 8 + (c & 7)).float() * (((c >> 3) - 1).clamp(min=0) + 127 << 23).view(torch.float32)
+    step = ((e - unit).clamp(1, 254) << 23).view(torch.float32)
+    return ((whole * sign).view(-1, GROUP) * step[:, None]).view(-1)
+
+
+def _hash(x):
+    """32 bits from 32 bits (int32 tensors, products modulo 2^32)."""
+    a, b = 0x6A09E667, 0xBB67AE85 - (1 << 32)
+    x = (x ^ (x >> 16 & 0xFFFF)) * a
+    x = (x ^ (x >> 15 & 0x1FFFF)) * b
+    return x ^ (x >> 16 & 0xFFFF)
+
+
+def _random(seed, n):
+    """Two numbers in [0, 1) of 16 bits for each of n elements."""
+    i32 = lambda v: torch.tensor((v & 0xFFFFFFFF) - ((v & 0x80000000) << 1), dtype=torch.int32, device="cuda")  # noqa: E731
+    key = _hash(_hash(i32((seed & 0xFFFFFFFF) + 0x3C6EF372)) ^ i32(seed >> 32))  # n is below 2^32
+    r = _hash(torch.arange(n, dtype=torch.int32, device="cuda") ^ key)
+    return (r & 0xFFFF).float() / 65536, (r >> 16 & 0xFFFF).float() / 65536
+
+
+def _encode8(x):
+    """The 8-bit form of activations, as values: codes of at most 127 steps, a power of two, the smallest that fits."""
+    v = x.reshape(-1, GROUP)
+    e = ((v.abs().amax(1).view(torch.int32) + 0x10000) >> 23).clamp(7, 254)
+    up, step = ((260 - e) << 23).view(torch.float32), ((e - 6) << 23).view(torch.float32)
+    return (torch.round(v * up[:, None]).clamp(-127, 127) * step[:, None]).view(x.shape)
+
+
+def _rows(c, v):
+    """A vector for every group -> for every row."""
+    return v if c["groups"] == 1 else v.repeat_interleave(c["group_rows"], 0)
+
+
+def _column_sums(c, x):
+    """The sum over each group's rows."""
+    return x.view(c["groups"], c["group_rows"], c["width"]).sum(1)
+
+
+def _plain_norm(s):
+    c = s["c"]
+    t, out = s["res"].dtype, {}
+    value = s["res"].float()
+    if c["residual"]:
+        value = value + (s["x"].float() * _rows(c, s["gate"]) if c["gate"] else s["x"].float())
+        out["sum"] = value.to(t)
+        value = out["sum"].float()
+    r = torch.rsqrt(value.square().mean(1, keepdim=True) + EPS)
+    hat = value * r
+    y = hat * _rows(c, s["scale"]) if c["scale"] else hat
+    if c["shift"]:
+        y = y + _rows(c, s["shift"])
+    y = y.to(t)
+    if c["eight"]:
+        out["back"] = _encode8(y.float()).to(torch.bfloat16)
+    else:
+        out["y"] = y
+    if c["kind"] == "step":
+        dy = s["dy"].float()
+        u = dy * _rows(c, s["scale"]) if c["scale"] else dy
+        h = r * (u - hat * (u * hat).mean(1, keepdim=True)) + s["dsum"].float()
+        out["dres"] = h.to(t)
+        if c["gate"]:
+            out["dx"] = (h * _rows(c, s["gate"])).to(t)
+            out["dgate"] = _column_sums(c, h * s["x"].float())
+        if c["scale"]:
+            out["dscale"] = _column_sums(c, dy * hat)
+        if c["shift"]:
+            out["dshift"] = _column_sums(c, dy)
+    return out
+
+
+def _plain_weights(s):
+    c, out, g = s["c"], {}, s["g"].float()
+    if s["norm"] is not None:
+        n = g.double().square().sum().sqrt()
+        out["norm"] = torch.stack([n, (s["most"] / n).clamp(max=1.0)]).float()
+        if c["kind"] == "gnorm":
+            return out
+        g = g * out["norm"][1]
+    s["step"] += 1
+    m, v = s["m"], s["v"]
+    if c["eight"]:
+        m, v = _decode(m, s["m_scales"], M_UNIT), _decode(v, s["v_scales"], V_UNIT)
+    m = BETA1 * m + (1 - BETA1) * g
+    v = BETA2 * v + (1 - BETA2) * g * g
+    root = v.sqrt() * (1 - BETA2 ** s["step"]) ** -0.5 + ADAM_EPS
+    s["p"] = s["p"] - (LR * DECAY * s["p"] + LR / (1 - BETA1 ** s["step"]) * m / root)
+    out["p"] = s["p"]
+    if c["copy"]:
+        out["copy"] = s["p"].to(torch.bfloat16)
+    if c["eight"]:
+        rm, rv = _random(s["step"], m.numel())
+        s["m"], s["m_scales"] = _encode(m, rm, M_UNIT)
+        s["v"], s["v_scales"] = _encode(v, rv, V_UNIT)
+        out["m"] = _decode(s["m"], s["m_scales"], M_UNIT).to(torch.bfloat16)
+        out["v"] = _decode(s["v"], s["v_scales"], V_UNIT).to(torch.bfloat16)
+    else:
+        s["m"], s["v"] = m, v
+        out["m"], out["v"] = m, v
+    return out
+
+
+# ---- the library's calls --------------------------------------------------------------
+
+def _own_norm(s):
+    from paper_2606_31248_amd import binding as B
+    c, out = s["c"], {}
+    desc = B.make_norm_desc(s["res"], group_rows=c["group_rows"], eps=EPS)
+    if c["eight"]:
+        B.strata_residual_norm(desc, s["x"], s["gate"], s["res"], s["scale"], s["shift"], s["sum"], None, s["codes"],
+                               s["scales"])
+        B.strata_ckpt_unpack(s["codes"], s["scales"], s["back"])
+        out["back"] = s["back"]
+    else:
+        B.strata_residual_norm(desc, s["x"], s["gate"], s["res"], s["scale"], s["shift"], s["sum"], s["y"])
+        out["y"] = s["y"]
+    if c["residual"]:
+        out["sum"] = s["sum"]
+    if c["kind"] == "step":
+        ws = torch.empty(B.strata_residual_norm_bwd_workspace_size(desc), dtype=torch.uint8, device="cuda")
+        total = s["sum"] if c["residual"] else s["res"]
+        B.strata_residual_norm_bwd(desc, total, s["x"] if c["gate"] else None, s["gate"], s["scale"], s["dy"], s["dsum"],
+                                   s["dres"], s["dx"], s["dgate"], s["dscale"], s["dshift"], ws)
+        out |= {n: s[n] for n in ("dres", "dx", "dgate", "dscale", "dshift") if s[n] is not None}
+    return out
+
+
+def _own_weights(s):
+    from paper_2606_31248_amd import binding as B
+    c, out = s["c"], {}
+    if s["norm"] is not None:
+        ws = torch.empty(B.strata_grad_norm_workspace_size(s["list"]), dtype=torch.uint8, device="cuda")
+        B.strata_grad_norm(s["list"], s["most"], s["norm"], ws)
+        out["norm"] = s["norm"]
+        if c["kind"] == "gnorm":
+            return out
+    s["step"] += 1
+    desc = B.make_adamw_desc(LR, s["step"], beta1=BETA1, beta2=BETA2, eps=ADAM_EPS, weight_decay=DECAY, seed=s["step"])
+    B.strata_adamw(desc, s["list"], s["m"], s["v"], s["m_scales"], s["v_scales"], s["norm"][1:] if c["clip"] else None)
+    out |= {"p": s["p"], "m": s["m"], "v": s["v"]}
+    if c["copy"]:
+        out["copy"] = s["copy"]
+    if c["eight"]:
+        B.strata_adamw_unpack(s["m"], s["m_scales"], s["m_values"], second=False)
+        B.strata_adamw_unpack(s["v"], s["v_scales"], s["v_values"], second=True)
+        out["m"], out["v"] = s["m_values"], s["v_values"]
+    return out
+
+
+def run(s):
+    norm = s["c"]["kind"] in ("norm", "step")
+    if own:
+        return _own_norm(s) if norm else _own_weights(s)
+    return _plain_norm(s) if norm else _plain_weights(s)
+
+
+def work(case):
+    c = case
+    if c["kind"] in ("norm", "step"):
+        e, n = 4 if c["dtype"] == "f32" else 2, c["groups"] * c["group_rows"] * c["width"]
+        vectors = 4 * c["groups"] * c["width"] * (c["gate"] + c["scale"] + c["shift"])
+        moved = n * e * (3 if c["residual"] else 1) + vectors              # x, residual, sum
+        # the 8 bits are written, and read again to be returned as values in 16
+        moved += n * (2 + 2 / GROUP + 2) if c["eight"] else n * e
+        if c["kind"] == "norm":
+            return {"bytes": moved, "flops": 8 * n}
+        # dy, dsum and the gradient of the stream, of the branch where it has a gate, of the vectors
+        return {"bytes": moved + n * e * (4 if c["gate"] else 3) + vectors, "flops": 24 * n}
+    n, e = sum(_sizes(c)), 4 if c["grads"] == "f32" else 2
+    if c["kind"] == "gnorm":
+        return {"bytes": n * e, "flops": 2 * n}
+    # the states read and written; in 8 bits also read and written as values in 16
+    states = 4 * (1 + 1 / GROUP) + 2 * (1 + 1 / GROUP + 2) if c["eight"] else 16
+    return {"bytes": n * (8 + e + states + (2 if c["copy"] else 0)), "flops": n * (60 if c["eight"] else 15)}
+
+
+# ---- the same results in 64 bits -------------------------------------------------------
+
+def _power(p):
+    """2^p in float64, exactly, for whole p from -1022 to 1023."""
+    return ((p.to(torch.int64) + 1023) << 52).view(torch.float64)
+
+
+def _held64(x):
+    """float64 values as the activations' 8 bits hold them."""
+    v = x.reshape(-1, GROUP)
+    top = v.abs().amax(1, keepdim=True)
+    p = torch.frexp(top)[1].to(torch.int64) - 7                # top = m 2^(p+7), 1/2 <= m < 1
+    p = torch.where(top * _power(-p) >= 127.5, p + 1, p).clamp(-126, 121)
+    return ((v * _power(-p)).round().clamp(-127, 127) * _power(p)).view(x.shape)
+
+
+def _state64(x, random, octaves):
+    """float64 states as 8 bits hold them: 3 bits behind the leading one, down to a smallest step of 2^-octaves times
+    the power of two of the group's largest, rounded up where the number in [0, 1) reaches over the border."""
+    v = x.view(-1, GROUP)
+    top = v.abs().amax(1, keepdim=True)
+    big = torch.frexp(top)[1].to(torch.int64) - 1
+    big = torch.where(top >= 1.875 * _power(big), big + 1, big)
+    a = v.abs()
+    own_power = torch.frexp(a)[1].to(torch.int64) - 1
+    step = _power(torch.maximum(own_power - 3, big - octaves))
+    held = torch.floor(a / step + random.view(-1, GROUP).double()) * step
+    if octaves == V_UNIT:
+        held = torch.where(a > 0, torch.maximum(held, _power(big - octaves).expand_as(held)), held)
+    return (torch.sign(v) * held).view(-1)
+
+
+def _bits64(seed, n):
+    """The two random numbers of each element, in 64-bit whole numbers."""
+    mask = 0xFFFFFFFF
+
+    def mix(x):
+        x = x ^ (x >> 16)
+        x = x * 0x6A09E667 & mask
+        x = x ^ (x >> 15)
+        x = x * 0xBB67AE85 & mask
+        return x ^ (x >> 16)
+
+    key = mix(mix((seed & mask) + 0x3C6EF372 & mask) ^ (seed >> 32))
+    r = mix(torch.arange(n, dtype=torch.int64, device="cuda") ^ key)
+    return (r % 65536).double() / 65536, (r // 65536).double() / 65536
+
+
+def _stream64(c, value, scale, shift):
+    y = value / (value.pow(2).sum(1, keepdim=True) / c["width"] + EPS).sqrt()
+    y = y if scale is None else y * scale
+    return y if shift is None else y + shift
+
+
+def _group64(c, s, b):
+    """What the rows of group b make, and for a step the gradients."""
+    t, out = s["res"].dtype, {}
+    rows = slice(b * c["group_rows"], (b + 1) * c["group_rows"])
+    gate, scale, shift = (None if s[n] is None else s[n][b].double() for n in ("gate", "scale", "shift"))
+    value = s["res"][rows].double()
+    if c["residual"]:
+        x = s["x"][rows].double()
+        value = value + (x if gate is None else gate * x)
+        out["sum"] = value
+        value = value.to(t).double()               # the norm is that of the sum as it is stored
+    y = _stream64(c, value, scale, shift)
+    if c["eight"]:
+        out["back"] = _held64(y.to(t).double())
+    else:
+        out["y"] = y
+    if c["kind"] != "step":
+        return out
+    value = value.detach().requires_grad_()
+    leaves = {n: v.detach().requires_grad_() for n, v in (("dscale", scale), ("dshift", shift)) if v is not None}
+    y = _stream64(c, value, leaves.get("dscale"), leaves.get("dshift"))
+    grads = torch.autograd.grad(y, [value] + list(leaves.values()), s["dy"][rows].double())
+    out.update(zip(leaves, grads[1:]))
+    out["dres"] = grads[0] + s["dsum"][rows].double()
+    if gate is not None:
+        out["dx"] = out["dres"] * gate
+        out["dgate"] = (out["dres"] * x).sum(0)
+    return out
+
+
+def _exact_weights(c, s):
+    g, out = s["g"].double(), {}
+    if s["norm"] is not None:
+        n = torch.linalg.vector_norm(g)
+        factor = torch.minimum(s["most"] / n, torch.ones_like(n))
+        out["norm"] = torch.stack([n, factor])
+        if c["kind"] == "gnorm":
+            return out
+        g = g * factor
+    k = STEP + 1
+    if c["eight"]:
+        m, v = (_decode(s[n], s[n + "_scales"], unit).double() for n, unit in (("m", M_UNIT), ("v", V_UNIT)))
+    else:
+        m, v = s["m"].double(), s["v"].double()
+    m = m + (g - m) * (1 - BETA1)
+    v = v + (g * g - v) * (1 - BETA2)
+    step = (m / (1 - BETA1 ** k)) / ((v / (1 - BETA2 ** k)).sqrt() + ADAM_EPS)
+    out["p"] = s["p"].double() * (1 - LR * DECAY) - LR * step
+    if c["copy"]:
+        out["copy"] = out["p"]
+    if c["eight"]:
+        rm, rv = _bits64(k, m.numel())
+        m, v = _state64(m, rm, M_UNIT), _state64(v, rv, V_UNIT)
+    out["m"], out["v"] = m, v
+    return out
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(case, seed)
+    if c["kind"] not in ("norm", "step"):
+        return _exact_weights(c, s)
+    parts = [_group64(c, s, b) for b in range(c["groups"])]
+    return {n: torch.stack([p[n] for p in parts]) if n in ("dgate", "dscale", "dshift") else torch.cat([p[n] for p in parts])
+            for n in parts[0]}
