@@ -198,9 +198,10 @@ def _exponent(bits):
 
 def _encode(x, random, unit):
     """float32 values and numbers in [0, 1) that decide their rounding -> codes and exponents of groups of 32.
-    A group's unit lies `unit` octaves below its largest's exponent; 3 bits behind the leading one, signed for M_UNIT."""
-    e = _exponent(x.abs().view(-1, GROUP).amax(1).view(torch.int32))
-    up = ((127 + unit + 127 - e).clamp(1, 254) << 23).view(torch.float32)
+    A group's unit lies `unit` octaves below its largest's exponent, at 2^-126 or above; 3 bits behind the leading one,
+    signed for M_UNIT."""
+    e = _exponent(x.abs().view(-1, GROUP).amax(1).view(torch.int32)).clamp(min=unit + 1)
+    up = ((254 + unit - e) << 23).view(torch.float32)
     t = (x.abs().view(-1, GROUP) * up[:, None]).view(-1)
     ex = ((t.view(torch.int32) >> 23) - 127).clamp(min=3)
     part = torch.floor(t * ((130 - ex) << 23).view(torch.float32) + random).to(torch.int32)
@@ -417,7 +418,7 @@ def _state64(x, random, octaves):
     v = x.view(-1, GROUP)
     top = v.abs().amax(1, keepdim=True)
     big = torch.frexp(top)[1].to(torch.int64) - 1
-    big = torch.where(top >= 1.875 * _power(big), big + 1, big)
+    big = torch.where(top >= 1.875 * _power(big), big + 1, big).clamp(min=octaves - 126)
     a = v.abs()
     own_power = torch.frexp(a)[1].to(torch.int64) - 1
     step = _power(torch.maximum(own_power - 3, big - octaves))
