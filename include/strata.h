@@ -10,6 +10,8 @@
  *   - the overlapping-tile stitch S = D^-1 P^T W and its extraction P
  *     (App. F, "Tile stitching", "Linear operator interpretation");
  *   - QK RMSNorm and the sigmoid output gate of the attention block (App. B.5);
+ *   - around the blocks in training: the residual stream's addition and RMS norm,
+ *     the norm of the gradients and AdamW over all weights (Sec. 4);
  *   - the wind vectors of each tile in its centre's East-North frame (Sec. 3.3,
  *     Eq. 2);
  *   - the Duo-grid halo padding across cube faces and the Kaiser-Bessel-derived
@@ -339,6 +341,122 @@ strata_status strata_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t*
                                void* stream);
 strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dtype,
                                  void* stream);
+
+/* ---- the residual stream between blocks: addition and RMS norm --------------
+ * How a block is entered (Sec. 3.2; conditioned as the decoder's blocks are): the branch
+ * that the block before made is added to the stream, and the sum's norm is what the next
+ * projection reads.  Rows of `width` contiguous elements, one a token; group_rows
+ * consecutive rows (a tile, or all rows) share a gate, a scale and a shift, float32
+ * [rows / group_rows, width] each, any of them NULL (gate and scale: 1, shift: 0):
+ *   sum = res + gate x  (rounded to dtype),   r = (mean_c sum_c^2 + eps)^(-1/2),
+ *   y   = r sum scale + shift  (rounded to dtype);
+ * without x (NULL; gate and sum then too) the norm is that of res.  y, or its 8-bit form
+ * (strata_ckpt_pack's of y, bit for bit: codes int8 [rows, width], scales uint8
+ * [rows, width / 32], for a width of whole 32), or both; what is not wanted is NULL.
+ * Arithmetic and sums in float32.  Range of the norm, here and in the backward: a row of
+ * root mean square 2^64 / sqrt(width) and more has squares that overflow, and a norm and
+ * a gradient of 0; with eps below 2^-126 a mean square below 2^-126 keeps fewer digits
+ * and one of 0 makes the row NaN.
+ * sum may be res or x itself; no other buffers may overlap. */
+typedef struct {
+  int64_t rows;       /* 1 to 2^31 - 1, rows * width below 2^40 */
+  int64_t group_rows; /* divides rows */
+  int32_t width;      /* 1 to 8192; a multiple of 8 is fastest */
+  float eps;          /* finite, >= 0 */
+  strata_dtype dtype; /* x, res, sum, y and the gradients of the rows */
+} strata_norm_desc;
+
+strata_status strata_residual_norm(const strata_norm_desc* desc, const void* x, const float* gate, const void* res,
+                                   const float* scale, const float* shift, void* sum, void* y, int8_t* codes,
+                                   uint8_t* scales, void* stream);
+
+/* The gradients, for dy = d/dy and dsum = d/dsum (what the stream's later uses gave; NULL:
+ * 0).  sum: the forward's (without x: its res).  With n = r sum, u = r scale dy:
+ *   dres = u - n mean_c(u_c n_c) + dsum,            dx = gate dres,
+ *   dscale = sum_t dy n,   dshift = sum_t dy,       dgate = sum_t dres x,
+ * sums over the rows t of a group, in float32 in a fixed order (deterministic); dres and dx
+ * rounded once, dgate of the unrounded dres.  Without a gate dx is dres (pass NULL); with
+ * one x, dx and dgate are needed.  dscale: needed with scale, NULL without; dshift: NULL if
+ * it is not wanted.  dgate, dscale, dshift: float32 [rows / group_rows, width], written.
+ * workspace: at least strata_residual_norm_bwd_workspace_size(desc) bytes (may be 0) where
+ * one of the three is wanted, else it may be NULL; calls in flight at once need one each.
+ * dres may be dsum or dy itself and dx may be x; no other buffers may overlap. */
+size_t strata_residual_norm_bwd_workspace_size(const strata_norm_desc* desc);
+strata_status strata_residual_norm_bwd(const strata_norm_desc* desc, const void* sum, const void* x, const float* gate,
+                                       const float* scale, const void* dy, const void* dsum, void* dres, void* dx,
+                                       float* dgate, float* dscale, float* dshift, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* ---- the update of the weights: norm of the gradients, AdamW ----------------
+ * A list of tensors: n elements each (0 allowed), float32 weights p, a gradient g of
+ * float32 or bf16 (NULL: none, the tensor is left as it is), and a bf16 copy of the
+ * weights for the model to use (NULL: none).  Device pointers, 16-byte aligned.  The
+ * states m and v of all tensors lie in one buffer each, in the list's order: tensor i
+ * takes n_i places from place_i, place_(i+1) = place_i + n_i rounded up to whole 32; the
+ * places between are zeros.  strata_params_table writes a table of the list into HOST
+ * memory of strata_params_bytes(tensors, count) bytes and fills *params but for `table`:
+ * the caller copies the bytes to the device, sets params->table to the copy and keeps it,
+ * the tensors and their addresses as long as the list is used.  p and copy may overlap
+ * neither each other nor a gradient. */
+typedef struct {
+  float* p;
+  const void* g;
+  uint16_t* copy;
+  int64_t n;
+  strata_dtype grad_dtype;
+} strata_param;
+
+typedef struct {
+  const void* table; /* DEVICE */
+  int64_t tensors;
+  int64_t chunks;    /* pieces of work */
+  int64_t places;    /* elements of each state */
+} strata_params;
+
+size_t strata_params_bytes(const strata_param* tensors, int64_t count); /* 0: a bad list */
+strata_status strata_params_table(const strata_param* tensors, int64_t count, void* table, size_t table_bytes,
+                                  strata_params* params);
+
+/* norm[0] = N, the square root of the sum of the squares of all gradients, norm[1] =
+ * min(1, max_norm / N): what clips them (1 for N = 0; NaN where a gradient is not finite).
+ * norm: float32 [2] on the device.  Sums in float64 in a fixed order; no gradient is too
+ * large or small for it (norm[0] itself rounds to float32).  max_norm > 0, infinity: no
+ * clipping.  workspace: strata_grad_norm_workspace_size(params) bytes (may be 0). */
+size_t strata_grad_norm_workspace_size(const strata_params* params);
+strata_status strata_grad_norm(const strata_params* params, double max_norm, float* norm, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Step number `step` (1 is the first) of AdamW on every tensor with a gradient: g' =
+ * factor g (factor: NULL or one float on the device, 4-byte aligned, e.g. norm + 1; NaN:
+ * nothing is changed),
+ *   m <- beta1 m + (1 - beta1) g',          v <- beta2 v + (1 - beta2) g'^2,
+ *   p <- p - lr (weight_decay p + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)),
+ * copy = p rounded.  In float32; m and v with every product and sum rounded by itself.
+ * States: float32 (m_scales, v_scales NULL), or 8 bits: m, v uint8 [places], scales uint8
+ * [places / 32], both zeros at the start, for lists of less than 2^32 places.  With E the
+ * group's scale: a code c of m has a sign (bit 7) and magnitude k = c mod 128, one of v the
+ * magnitude k = c, and stands for f(k) 2^(max(E - U, 1) - 127), U = 17 (m) or 33 (v), f(k) =
+ * k below 8 and (8 + k mod 8) 2^(k div 8 - 1) above: 3 bits behind the leading one down to 8
+ * units.  E is the biased exponent of the group's largest value after the step (one more
+ * from 1.875 times the power of two on), at least U + 1.  A value is rounded to one of its
+ * two neighbours, up with the probability of its distance to the lower, so that a state
+ * moves by less than a code's step (beta2 = 0.999 moves v by a thousandth) in the mean as it
+ * should; v above 0 keeps at least code 1.  The random numbers are a hash of (seed, place):
+ * give every step another seed.  A group with an infinity or a NaN has scale 255 and codes
+ * 0 and stands for 32 NaN.
+ * lr, step and seed are of the call: a captured call repeats them. */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* >= 0, beta < 1, eps >= 2^-126, finite */
+  int64_t step;                               /* >= 1 */
+  uint64_t seed;                              /* of the 8-bit states' rounding */
+} strata_adamw_desc;
+
+strata_status strata_adamw(const strata_adamw_desc* desc, const strata_params* params, void* m, void* v,
+                           uint8_t* m_scales, uint8_t* v_scales, const float* factor, void* stream);
+
+/* The values of 8-bit states (second: v), exact in bf16 too: x [n] of dtype, 1 <= n < 2^32. */
+strata_status strata_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t second, void* x,
+                                  strata_dtype dtype, void* stream);
 
 /* ---- a8: tile stitch S = D^-1 P^T W (App. F, Eq. stitch) -------------------
  * Regular tiling: tile t = a*ntx + b has origin (a*stride_y, b*stride_x) on the

@@ -31,6 +31,9 @@ EXPORTS = (
     "strata_duo_pad_vjp", "strata_na3d_fwd_stitch", "strata_tile_blend_overlap", "strata_na3d_bwd_noalloc",
     "strata_qkv_heads", "strata_qkv_heads_ckpt", "strata_qkv_heads_bwd_workspace_size", "strata_qkv_heads_bwd",
     "strata_ckpt_pack", "strata_ckpt_unpack",
+    "strata_residual_norm", "strata_residual_norm_bwd_workspace_size", "strata_residual_norm_bwd",
+    "strata_params_bytes", "strata_params_table", "strata_grad_norm_workspace_size", "strata_grad_norm",
+    "strata_adamw", "strata_adamw_unpack",
     "strata_status_string", "strata_last_error",
 )
 
@@ -68,6 +71,26 @@ class QKVDesc(ctypes.Structure):
     def width(self) -> int:
         """Elements of a row: q, k, v and the gate's logits."""
         return self.kept + (self.heads if self.gate_dim == 1 else 0)
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("group_rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+class ParamEntry(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("grad_dtype", ctypes.c_int)]
+
+
+class ParamList(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("tensors", ctypes.c_int64), ("chunks", ctypes.c_int64),
+                ("places", ctypes.c_int64)]
+
+
+class AdamWDesc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
 
 
 _lib = None
@@ -126,6 +149,23 @@ def load(path: str = LIB_PATH):
         f = getattr(L, name)
         f.argtypes = args
         f.restype = st
+    N, E, PL = ctypes.POINTER(NormDesc), ctypes.POINTER(ParamEntry), ctypes.POINTER(ParamList)
+    for name, args in {
+        "strata_residual_norm": [N, P, P, P, P, P, P, P, P, P, P],
+        "strata_residual_norm_bwd": [N, P, P, P, P, P, P, P, P, P, P, P, P, size, P],
+        "strata_params_table": [E, i64, P, size, PL],
+        "strata_grad_norm": [PL, ctypes.c_double, P, P, size, P],
+        "strata_adamw": [ctypes.POINTER(AdamWDesc), PL, P, P, P, P, P, P],
+        "strata_adamw_unpack": [P, P, i64, i32, P, st, P],
+    }.items():
+        f = getattr(L, name)
+        f.argtypes = args
+        f.restype = st
+    for name, args in {"strata_residual_norm_bwd_workspace_size": [N], "strata_params_bytes": [E, i64],
+                       "strata_grad_norm_workspace_size": [PL]}.items():
+        f = getattr(L, name)
+        f.argtypes = args
+        f.restype = size
     L.strata_qkv_heads_bwd_workspace_size.argtypes = [Q]
     L.strata_qkv_heads_bwd_workspace_size.restype = size
     L.strata_na3d_bwd_workspace_size.argtypes = [D]
@@ -597,3 +637,165 @@ def strata_ckpt_unpack(codes, scales, x, stream=None):
     """The values of codes and scales into x."""
     n, px, pc, ps = _ckpt_args(x, codes, scales)
     _check(load().strata_ckpt_unpack(pc, ps, n, px, _dtype(x), _on(x.device, stream)))
+
+
+# ---- the residual stream's norm; the update of the weights -----------------------
+
+def make_norm_desc(rows, group_rows: Optional[int] = None, eps: float = 1e-6) -> NormDesc:
+    """Of a tensor [..., width], a row for each of the places before: group_rows consecutive rows share a gate, a
+    scale and a shift (default: all)."""
+    width = rows.shape[-1] if rows.dim() else 0
+    many = rows.numel() // width if width else 0
+    return NormDesc(many, many if group_rows is None else group_rows, width, float(eps), _dtype(rows))
+
+
+def _norm_at(desc: NormDesc, dev, dt, **tensors):
+    """Addresses of tensors of rows * width elements of dtype `dt` on `dev`, None for None."""
+    n, width = desc.rows * desc.width, desc.width
+    out = []
+    for name, t in tensors.items():
+        if t is None:
+            out.append(None)
+            continue
+        if not (type(t) is torch.Tensor and t.dtype is dt and t.device == dev and t.is_contiguous() and t.numel() == n
+                and t.shape[-1] == width):
+            _need(name, t, None, dt, dev)
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {desc.rows} rows of {width}")
+        out.append(t.data_ptr())
+    return out
+
+
+def _vectors_at(desc: NormDesc, dev, **vectors):
+    """Addresses of float32 [groups, width] ([width] for a single group), None for None."""
+    groups, width = desc.rows // max(desc.group_rows, 1), desc.width
+    return [None if t is None else
+            _at(name, t, (width,) if groups == 1 and getattr(t, "ndim", 0) == 1 else (groups, width), torch.float32, dev)
+            for name, t in vectors.items()]
+
+
+def _norm_common(desc: NormDesc, name, t):
+    dt = _torch_dtype(desc.dtype)
+    if not (type(t) is torch.Tensor and t.is_cuda and t.dtype is dt):
+        _need(name, t, None, dt)
+    return dt, t.device
+
+
+def strata_residual_norm(desc: NormDesc, x, gate, res, scale, shift, sum, y=None, codes=None, scales=None, stream=None):
+    """sum = res + gate x, y = its RMS norm with scale and shift, and / or y in 8 bits (codes int8 of y's shape,
+    scales uint8 of a 32nd of its elements).  Without x (gate and sum None) the norm of res."""
+    dt, dev = _norm_common(desc, "res", res)
+    px, pres, psum, py = _norm_at(desc, dev, dt, x=x, res=res, sum=sum, y=y)
+    pcodes, = _norm_at(desc, dev, torch.int8, codes=codes)
+    if scales is not None:
+        _need("scales", scales, None, torch.uint8, dev)
+        if scales.numel() != desc.rows * desc.width // 32:
+            raise ValueError(f"scales: {scales.numel()} elements, expected {desc.rows * desc.width // 32}")
+    pgate, pscale, pshift = _vectors_at(desc, dev, gate=gate, scale=scale, shift=shift)
+    _check(load().strata_residual_norm(ctypes.byref(desc), px, pgate, pres, pscale, pshift, psum, py, pcodes, _ptr(scales),
+                                       _on(dev, stream)))
+
+
+def strata_residual_norm_bwd_workspace_size(desc: NormDesc) -> int:
+    return int(load().strata_residual_norm_bwd_workspace_size(ctypes.byref(desc)))
+
+
+def strata_residual_norm_bwd(desc: NormDesc, sum, x, gate, scale, dy, dsum, dres, dx=None, dgate=None, dscale=None,
+                             dshift=None, workspace=None, stream=None):
+    """Gradients dres (and dx, with a gate) of the rows and dgate, dscale, dshift of the vectors for dy and dsum."""
+    dt, dev = _norm_common(desc, "sum", sum)
+    psum, px, pdy, pdsum, pdres, pdx = _norm_at(desc, dev, dt, sum=sum, x=x, dy=dy, dsum=dsum, dres=dres, dx=dx)
+    pgate, pscale, pdgate, pdscale, pdshift = _vectors_at(desc, dev, gate=gate, scale=scale, dgate=dgate, dscale=dscale,
+                                                          dshift=dshift)
+    _need("workspace", workspace, device=dev, optional=True)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().strata_residual_norm_bwd(ctypes.byref(desc), psum, px, pgate, pscale, pdy, pdsum, pdres, pdx, pdgate,
+                                           pdscale, pdshift, _ptr(workspace), nbytes, _on(dev, stream)))
+
+
+class Params:
+    """A list of weights with their gradients and copies (make_params).  places: elements of each state of AdamW,
+    at: the first of each tensor's."""
+
+    def __init__(self, tensors, desc, table, at, device):
+        self.tensors, self.desc, self.table, self.at, self.device = tensors, desc, table, at, device  # tensors: kept alive
+
+    @property
+    def places(self) -> int:
+        return self.desc.places
+
+
+def make_params(p, g, copies=None) -> Params:
+    """float32 weights, their gradients (float32 or bf16; None: the tensor is left as it is) and, for a model that
+    computes in it, bf16 copies of the weights (None: no copy).  The list holds the tensors' addresses: it is made
+    again when one of them moves."""
+    p, g = list(p), list(g)
+    copies = [None] * len(p) if copies is None else list(copies)
+    if not p or len(g) != len(p) or len(copies) != len(p):
+        raise ValueError(f"make_params: {len(p)} weights, {len(g)} gradients, {len(copies)} copies")
+    dev, entries, at, place = None, (ParamEntry * len(p))(), [], 0
+    for i, (w, d, c) in enumerate(zip(p, g, copies)):
+        _need(f"p[{i}]", w, None, torch.float32, dev)
+        dev = w.device
+        if d is not None:
+            _need(f"g[{i}]", d, w.shape, None, dev)
+            _dtype(d)
+        if c is not None:
+            _need(f"copies[{i}]", c, w.shape, torch.bfloat16, dev)
+        n = w.numel()
+        entries[i] = ParamEntry(w.data_ptr() if n else None, None if d is None or not n else d.data_ptr(),
+                                None if c is None or not n else c.data_ptr(), n,
+                                STRATA_F32 if d is None else _dtype(d))
+        at.append(place)
+        place += (n + 31) // 32 * 32
+    nbytes, desc = int(load().strata_params_bytes(entries, len(p))), ParamList()
+    table = torch.empty(max(nbytes, 1), dtype=torch.uint8)
+    _check(load().strata_params_table(entries, len(p), table.data_ptr(), nbytes, ctypes.byref(desc)))
+    table = table.to(dev)
+    desc.table = table.data_ptr()
+    return Params((p, g, copies), desc, table, at, dev)
+
+
+def strata_grad_norm_workspace_size(params: Params) -> int:
+    return int(load().strata_grad_norm_workspace_size(ctypes.byref(params.desc)))
+
+
+def strata_grad_norm(params: Params, max_norm, norm, workspace, stream=None):
+    """norm (float32 [2]): the norm of all gradients and the factor that brings it to max_norm at most."""
+    dev = params.device
+    at = _at("norm", norm, (2,), torch.float32, dev)
+    _need("workspace", workspace, device=dev, optional=True)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().strata_grad_norm(ctypes.byref(params.desc), max_norm, at, _ptr(workspace), nbytes, _on(dev, stream)))
+
+
+def make_adamw_desc(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0) -> AdamWDesc:
+    """Step number `step` (1 is the first); seed: of the rounding of states in 8 bits, another every step."""
+    return AdamWDesc(lr, beta1, beta2, eps, weight_decay, step, seed % (1 << 64))
+
+
+def strata_adamw(desc: AdamWDesc, params: Params, m, v, m_scales=None, v_scales=None, factor=None, stream=None):
+    """One step on every tensor of the list that has a gradient.  m, v: float32 [places], or uint8 with scales
+    uint8 [places / 32]; factor: float32 [1], what the gradients are multiplied by (NaN: nothing is changed)."""
+    dev, n = params.device, params.places
+    eight = m_scales is not None or v_scales is not None
+    dt = torch.uint8 if eight else torch.float32
+    for name, t in (("m", m), ("v", v)) + ((("m_scales", m_scales), ("v_scales", v_scales)) if eight else ()):
+        _like(name, t, (n // 32,) if name.endswith("scales") else (n,), dt, dev)
+    if factor is not None:
+        _like("factor", factor, (1,), torch.float32, dev)
+    at = [None if t is None or not n else t.data_ptr() for t in (m, v, m_scales, v_scales)]
+    _check(load().strata_adamw(ctypes.byref(desc), ctypes.byref(params.desc), *at,
+                               None if factor is None else factor.data_ptr(), _on(dev, stream)))
+
+
+def strata_adamw_unpack(codes, scales, values, second, stream=None):
+    """The values of states in 8 bits (second: of v): any whole number of groups of 32, and of the last a part."""
+    if not (type(values) is torch.Tensor and values.is_cuda and values.is_contiguous()):
+        _need("values", values)
+    n, dev = values.numel(), values.device
+    for name, t, many in (("codes", codes, n), ("scales", scales, (n + 31) // 32)):
+        _need(name, t, None, torch.uint8, dev)
+        if t.numel() != many:
+            raise ValueError(f"{name}: {t.numel()} elements, expected {many}")
+    _check(load().strata_adamw_unpack(codes.data_ptr(), scales.data_ptr(), n, int(bool(second)), values.data_ptr(),
+                                      _dtype(values), _on(dev, stream)))

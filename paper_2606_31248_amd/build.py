@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libstrata.so")
 
 SOURCES = ["api.hip", "geometry.hip", "rope.hip", "blend.hip", "na3d_any.hip", "na3d_opts.hip", "na3d_col.hip", "duo.hip", "na3d_mfma_q.hip",
            "na3d_mfma_kv.hip", "na3d_mfma_kvp.hip", "na3d_fwd_zs.hip", "na3d_fwd_lsg.hip", "na3d_mfma_d128.hip",
-           "na3d_bwd_d128.hip", "qkv_heads.hip", "ckpt8.hip"]
+           "na3d_bwd_d128.hip", "qkv_heads.hip", "ckpt8.hip", "row_norm.hip", "adamw.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

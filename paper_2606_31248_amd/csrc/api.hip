@@ -4,7 +4,9 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
+#include <new>
 
 #include "common.h"
 #include "kernels.h"
@@ -363,6 +365,72 @@ static strata_status check_qkv_weights(const strata_qkv_desc* d, const float* wq
 
 using namespace strata;
 
+static strata_status check_norm(const strata_norm_desc* d, NormArgs* a) {
+  REQUIRE(d, "desc: null pointer");
+  REQUIRE(d->rows > 0 && d->rows <= INT32_MAX && d->width > 0, "norm: need 1 <= rows < 2^31 and a width (rows=%lld, width=%d)",
+          (long long)d->rows, d->width);
+  REQUIRE(d->group_rows > 0 && d->rows % d->group_rows == 0, "norm: group_rows (%lld) must divide rows (%lld)",
+          (long long)d->group_rows, (long long)d->rows);
+  REQUIRE(isfinite(d->eps) && d->eps >= 0.f, "norm: eps must be finite and >= 0");
+  REQUIRE(d->dtype == STRATA_F32 || d->dtype == STRATA_BF16, "norm: unknown dtype %d", (int)d->dtype);
+  if (d->width > kMaxNormWidth)
+    return set_error(STRATA_ERR_UNSUPPORTED, "norm: width %d not supported (at most %d)", d->width, kMaxNormWidth);
+  REQUIRE(d->rows * d->width < kMaxElems, "norm: tensor too large");
+  a->rows = d->rows, a->group_rows = d->group_rows, a->groups = d->rows / d->group_rows;
+  a->width = d->width, a->eps = d->eps;
+  return STRATA_OK;
+}
+
+static int64_t places_of(const strata_param& t) { return (t.n + 31) / 32 * 32; }
+static int64_t chunks_of(const strata_param& t) { return t.g ? (t.n + kParamChunk - 1) / kParamChunk : 0; }
+static size_t table_bytes_of(const strata_params& p) {
+  return (p.tensors * sizeof(ParamRecord) + p.chunks * sizeof(int32_t) + 15) & ~(size_t)15;
+}
+
+// A list's sizes; refuses what is written through two of its pointers, or written and read.
+static strata_status check_params(const strata_param* t, int64_t count, strata_params* p) {
+  REQUIRE(t, "tensors: null pointer");
+  REQUIRE(count > 0 && count <= INT32_MAX / 4, "params: need 1 to 2^29 tensors (%lld)", (long long)count);
+  *p = strata_params{nullptr, count, 0, 0};
+  for (int64_t i = 0; i < count; ++i) {
+    REQUIRE(t[i].n >= 0 && t[i].n < kMaxElems, "params: tensor %lld has %lld elements", (long long)i, (long long)t[i].n);
+    REQUIRE(t[i].grad_dtype == STRATA_F32 || t[i].grad_dtype == STRATA_BF16, "params: unknown dtype %d", (int)t[i].grad_dtype);
+    REQUIRE(t[i].p || !t[i].n, "params: tensor %lld is a null pointer", (long long)i);
+    REQUIRE(aligned16(t[i].p) && aligned16(t[i].g) && aligned16(t[i].copy),
+            "params: tensor %lld, its gradient or copy: not 16-byte aligned", (long long)i);
+    p->chunks += chunks_of(t[i]);
+    p->places += places_of(t[i]);
+    REQUIRE(p->places < kMaxElems && p->chunks <= INT32_MAX, "params: too many elements");
+  }
+  struct Span {
+    uintptr_t from, to;
+    bool written;
+  };
+  Span* s = new (std::nothrow) Span[3 * count];
+  if (!s) return set_error(STRATA_ERR_WORKSPACE, "params: no host memory for %lld tensors", (long long)count);
+  int64_t many = 0;
+  auto add = [&](const void* q, int64_t bytes, bool written) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(q);
+    if (q && bytes) s[many++] = Span{from, from + (uintptr_t)bytes, written};
+  };
+  for (int64_t i = 0; i < count; ++i) {
+    add(t[i].p, 4 * t[i].n, true);
+    add(t[i].copy, 2 * t[i].n, true);
+    add(t[i].g, (t[i].grad_dtype == STRATA_BF16 ? 2 : 4) * t[i].n, false);
+  }
+  std::sort(s, s + many, [](const Span& a, const Span& b) { return a.from < b.from; });
+  bool apart = true;
+  uintptr_t end = 0, written_end = 0;  // of all spans so far, of the written ones
+  for (int64_t i = 0; i < many; ++i) {
+    apart = apart && s[i].from >= (s[i].written ? end : written_end);
+    end = std::max(end, s[i].to);
+    if (s[i].written) written_end = std::max(written_end, s[i].to);
+  }
+  delete[] s;
+  REQUIRE(apart, "params: weights and copies may overlap neither each other nor a gradient (a tensor twice?)");
+  return STRATA_OK;
+}
+
 extern "C" {
 
 const char* strata_status_string(strata_status st) {
@@ -607,6 +675,163 @@ strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int
   REQUIRE_PTR(x);
   launch_ckpt_unpack(codes, scales, n, x, dtype, (hipStream_t)stream);
   return check_launch("strata_ckpt_unpack");
+}
+
+strata_status strata_residual_norm(const strata_norm_desc* desc, const void* x, const float* gate, const void* res,
+                                   const float* scale, const float* shift, void* sum, void* y, int8_t* codes,
+                                   uint8_t* scales, void* stream) {
+  NormArgs a;
+  strata_status st = check_norm(desc, &a);
+  if (st != STRATA_OK) return st;
+  REQUIRE_PTR(res);
+  REQUIRE(!sum == !x, "sum: needed with x and NULL without");
+  REQUIRE(x || !gate, "gate: without x there is nothing to gate");
+  REQUIRE(aligned16(x) && aligned16(sum), "x, sum: not 16-byte aligned");
+  REQUIRE(aligned16(gate) && aligned16(scale) && aligned16(shift), "gate, scale, shift: not 16-byte aligned");
+  REQUIRE(!codes == !scales, "codes, scales: both or neither");
+  REQUIRE(y || codes, "y, codes: one of them is needed");
+  REQUIRE(aligned16(y) && aligned16(codes) && aligned16(scales), "y, codes, scales: not 16-byte aligned");
+  REQUIRE(!codes || desc->width % 32 == 0, "codes: the width %d is no multiple of 32", desc->width);
+  a.x = x, a.gate = gate, a.res = res, a.scale = scale, a.shift = shift;
+  a.sum = sum, a.y = y, a.codes = codes, a.scales = scales;
+  launch_residual_norm(a, desc->dtype, (hipStream_t)stream);
+  return check_launch("strata_residual_norm");
+}
+
+size_t strata_residual_norm_bwd_workspace_size(const strata_norm_desc* desc) {
+  NormArgs a;
+  if (check_norm(desc, &a) != STRATA_OK) return 0;
+  return (residual_norm_partial_bytes(a) + 255) & ~(size_t)255;
+}
+
+strata_status strata_residual_norm_bwd(const strata_norm_desc* desc, const void* sum, const void* x, const float* gate,
+                                       const float* scale, const void* dy, const void* dsum, void* dres, void* dx,
+                                       float* dgate, float* dscale, float* dshift, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  NormArgs a;
+  strata_status st = check_norm(desc, &a);
+  if (st != STRATA_OK) return st;
+  REQUIRE_PTR(sum);
+  REQUIRE_PTR(dy);
+  REQUIRE_PTR(dres);
+  REQUIRE(!x == !gate && !dx == !gate && !dgate == !gate, "x, dx, dgate: needed with gate and NULL without");
+  REQUIRE(!dscale == !scale, "dscale: needed with scale and NULL without");
+  REQUIRE(aligned16(x) && aligned16(gate) && aligned16(scale) && aligned16(dsum) && aligned16(dx),
+          "x, gate, scale, dsum, dx: not 16-byte aligned");
+  REQUIRE(aligned16(dgate) && aligned16(dscale) && aligned16(dshift), "dgate, dscale, dshift: not 16-byte aligned");
+  if (dgate || dscale || dshift) {
+    const size_t need = residual_norm_partial_bytes(a);
+    if (need && (!workspace || workspace_bytes < need))
+      return set_error(STRATA_ERR_WORKSPACE, "workspace: %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+    REQUIRE(aligned16(workspace), "workspace: not 16-byte aligned");
+    a.partial = static_cast<float*>(workspace);
+  }
+  a.total = sum, a.x = x, a.gate = gate, a.scale = scale, a.dy = dy, a.dsum = dsum;
+  a.dres = dres, a.dx = dx, a.dgate = dgate, a.dscale = dscale, a.dshift = dshift;
+  launch_residual_norm_bwd(a, desc->dtype, (hipStream_t)stream);
+  return check_launch("strata_residual_norm_bwd");
+}
+
+size_t strata_params_bytes(const strata_param* tensors, int64_t count) {
+  strata_params p;
+  return check_params(tensors, count, &p) == STRATA_OK ? table_bytes_of(p) : 0;
+}
+
+strata_status strata_params_table(const strata_param* tensors, int64_t count, void* table, size_t table_bytes,
+                                  strata_params* params) {
+  strata_params p;
+  strata_status st = check_params(tensors, count, &p);
+  if (st != STRATA_OK) return st;
+  REQUIRE(params, "params: null pointer");
+  REQUIRE(table && reinterpret_cast<uintptr_t>(table) % alignof(ParamRecord) == 0, "table: null or not 8-byte aligned");
+  if (table_bytes < table_bytes_of(p))
+    return set_error(STRATA_ERR_WORKSPACE, "table: %zu bytes, %zu needed", table_bytes, table_bytes_of(p));
+  ParamRecord* r = static_cast<ParamRecord*>(table);
+  int32_t* owner = reinterpret_cast<int32_t*>(r + count);
+  int64_t place = 0, chunk = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const strata_param& t = tensors[i];
+    r[i] = {t.p, t.g, t.copy, t.n, place, chunk, t.grad_dtype == STRATA_BF16};
+    for (int64_t k = chunks_of(t); k > 0; --k) owner[chunk++] = (int32_t)i;
+    place += places_of(t);
+  }
+  *params = p;
+  return STRATA_OK;
+}
+
+static strata_status check_list(const strata_params* p) {
+  REQUIRE(p, "params: null pointer");
+  REQUIRE_PTR(p->table);
+  REQUIRE(p->tensors > 0 && p->tensors <= INT32_MAX && p->chunks >= 0 && p->chunks <= INT32_MAX && p->places >= 0 &&
+              p->places < kMaxElems,
+          "params: not what strata_params_table filled");
+  return STRATA_OK;
+}
+static const ParamRecord* records(const strata_params* p) { return static_cast<const ParamRecord*>(p->table); }
+static const int32_t* owners(const strata_params* p) { return reinterpret_cast<const int32_t*>(records(p) + p->tensors); }
+
+size_t strata_grad_norm_workspace_size(const strata_params* params) {
+  if (check_list(params) != STRATA_OK) return 0;
+  return (grad_norm_blocks(params->chunks) * sizeof(double) + 255) & ~(size_t)255;
+}
+
+strata_status strata_grad_norm(const strata_params* params, double max_norm, float* norm, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  strata_status st = check_list(params);
+  if (st != STRATA_OK) return st;
+  REQUIRE(max_norm > 0., "grad norm: max_norm must be > 0");
+  REQUIRE_PTR(norm);
+  const size_t need = grad_norm_blocks(params->chunks) * sizeof(double);
+  if (need && (!workspace || workspace_bytes < need))
+    return set_error(STRATA_ERR_WORKSPACE, "workspace: %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+  REQUIRE(aligned16(workspace), "workspace: not 16-byte aligned");
+  launch_grad_norm(records(params), owners(params), params->chunks, max_norm, norm, static_cast<double*>(workspace),
+                   (hipStream_t)stream);
+  return check_launch("strata_grad_norm");
+}
+
+strata_status strata_adamw(const strata_adamw_desc* d, const strata_params* params, void* m, void* v,
+                           uint8_t* m_scales, uint8_t* v_scales, const float* factor, void* stream) {
+  REQUIRE(d, "desc: null pointer");
+  REQUIRE(d->lr >= 0. && isfinite(d->lr) && d->weight_decay >= 0. && isfinite(d->weight_decay),
+          "adamw: lr and weight_decay must be finite and >= 0");
+  REQUIRE(d->beta1 >= 0. && d->beta1 < 1. && d->beta2 >= 0. && d->beta2 < 1., "adamw: betas must lie in [0, 1)");
+  REQUIRE(d->eps >= 0x1p-126 && isfinite((float)d->eps), "adamw: eps must lie between 2^-126 and float32's largest");
+  REQUIRE(d->step >= 1, "adamw: steps count from 1 (step=%lld)", (long long)d->step);
+  strata_status st = check_list(params);
+  if (st != STRATA_OK) return st;
+  REQUIRE(!m_scales == !v_scales, "m_scales, v_scales: both or neither");
+  if (params->places) {
+    REQUIRE_PTR(m);
+    REQUIRE_PTR(v);
+  }
+  REQUIRE(aligned16(m_scales) && aligned16(v_scales), "m_scales, v_scales: not 16-byte aligned");
+  REQUIRE(reinterpret_cast<uintptr_t>(factor) % 4 == 0, "factor: not 4-byte aligned");
+  REQUIRE(!m_scales || params->places < ((int64_t)1 << 32), "adamw: states in 8 bits have less than 2^32 places");
+  AdamArgs a;
+  a.tensors = records(params), a.owner = owners(params), a.chunks = params->chunks;
+  a.m = m, a.v = v, a.m_scales = m_scales, a.v_scales = v_scales, a.factor = factor;
+  a.beta1 = (float)d->beta1, a.new1 = (float)(1. - d->beta1), a.beta2 = (float)d->beta2, a.new2 = (float)(1. - d->beta2);
+  a.rate = (float)(d->lr / (1. - pow(d->beta1, (double)d->step)));
+  a.decay = (float)(d->lr * d->weight_decay);
+  a.root = (float)(1. / sqrt(1. - pow(d->beta2, (double)d->step)));
+  a.eps = (float)d->eps;
+  REQUIRE(isfinite(a.rate) && isfinite(a.decay) && isfinite(a.root), "adamw: lr and betas beyond float32's range");
+  a.key = adamw_key(d->seed);
+  if (!params->chunks) return STRATA_OK;  // no tensor has a gradient
+  launch_adamw(a, (hipStream_t)stream);
+  return check_launch("strata_adamw");
+}
+
+strata_status strata_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t second, void* x,
+                                  strata_dtype dtype, void* stream) {
+  REQUIRE(n > 0 && n < ((int64_t)1 << 32), "adamw: need 1 <= n < 2^32 (n=%lld)", (long long)n);
+  REQUIRE(dtype == STRATA_F32 || dtype == STRATA_BF16, "adamw: unknown dtype %d", (int)dtype);
+  REQUIRE_PTR(codes);
+  REQUIRE_PTR(scales);
+  REQUIRE_PTR(x);
+  launch_adamw_unpack(codes, scales, n, second != 0, x, dtype, (hipStream_t)stream);
+  return check_launch("strata_adamw_unpack");
 }
 
 static strata_status check_tiling(int32_t nty, int32_t ntx, int32_t P, int32_t Ht, int32_t Wt,

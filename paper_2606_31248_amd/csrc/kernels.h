@@ -34,13 +34,28 @@ void launch_rope_phases(const float* coords, int B, int H, int W, int head_dim, 
 void launch_rope_apply(const void* x, void* y, const float* cs, int B, int heads, int Z, int H,
                        int W, int head_dim, strata_dtype dt, int transpose, hipStream_t s);
 
+// Division by a number known at the launch: n / d for n < 2^31 (d = 1: no multiplier).
+// mul = ceil(2^(31 + l) / d), 2^l >= d, so that n mul / 2^(31 + l) is less than 1/d above n / d.
+struct FastDiv {
+  uint32_t mul = 0, shift = 0;  // n / d = mulhi(n, mul) >> shift; mul = 0: d = 1
+};
+inline FastDiv fast_div(int64_t d) {
+  FastDiv f;
+  if (d == 1) return f;
+  int l = 1;
+  while (((int64_t)1 << l) < d) ++l;
+  f.mul = (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d);
+  f.shift = l - 1;
+  return f;
+}
+__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& d) {
+  return d.mul ? __umulhi(n, d.mul) >> d.shift : n;
+}
+
 // Projection rows and the head layout (qkv_heads.hip).  A row is cut into `slices`
 // pieces of head_dim channels (heads of q, kv of k, kv of v, and with gate_dim > 1
 // heads of the gate); with gate_dim == 1 the gate's `heads` logits follow.  The
 // backward reads dq, dk, dv, dgate through q, k, v, gate.
-struct FastDiv {
-  uint32_t mul = 0, shift = 0;  // n / d = mulhi(n, mul) >> shift for n < 2^31; mul = 0: d = 1
-};
 struct QkvArgs {
   const void* rows = nullptr;       // or, with codes, their 8-bit form
   const int8_t* codes = nullptr;
@@ -72,6 +87,57 @@ void launch_qkv_heads_bwd(QkvArgs a, int head_dim, strata_dtype dt, float* dwq, 
 void launch_ckpt_pack(const void* x, int64_t n, int8_t* codes, uint8_t* scales, strata_dtype dt, hipStream_t s);
 void launch_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int64_t n, void* x, strata_dtype dt,
                         hipStream_t s);
+
+// The residual stream's addition with its RMS norm, and the gradients (row_norm.hip).
+constexpr int kMaxNormWidth = 8192;
+struct NormArgs {
+  const void *x = nullptr, *res = nullptr, *total = nullptr, *dy = nullptr, *dsum = nullptr;
+  const float *gate = nullptr, *scale = nullptr, *shift = nullptr;
+  void *sum = nullptr, *y = nullptr, *dres = nullptr, *dx = nullptr;
+  int8_t* codes = nullptr;
+  uint8_t* scales = nullptr;
+  float *dgate = nullptr, *dscale = nullptr, *dshift = nullptr;
+  float* partial = nullptr;         // [vectors with a gradient][groups * chunks][width]
+  int64_t rows = 0, group_rows = 0, groups = 0;
+  int width = 0;
+  float eps = 0.f;
+  // the launch: forward, rows that a team takes; backward, blocks and rows of a block of one group
+  int steps = 1;
+  int64_t chunks = 0, span = 0;
+  FastDiv by_group;
+};
+void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s);
+size_t residual_norm_partial_bytes(NormArgs a);
+void launch_residual_norm_bwd(NormArgs a, strata_dtype dt, hipStream_t s);
+
+// AdamW over many tensors (adamw.hip).  The table on the device: one record a tensor, then the
+// tensor's index for every chunk of kParamChunk elements of the tensors with a gradient.
+constexpr int kParamChunk = 2048;
+struct ParamRecord {
+  float* p;
+  const void* g;
+  uint16_t* copy;
+  int64_t n, place, chunk;          // elements, first place in the states, first chunk
+  int64_t bf16;                     // type of g
+};
+struct AdamArgs {
+  const ParamRecord* tensors = nullptr;
+  const int32_t* owner = nullptr;   // of each chunk
+  int64_t chunks = 0;
+  void *m = nullptr, *v = nullptr;
+  uint8_t *m_scales = nullptr, *v_scales = nullptr;
+  const float* factor = nullptr;    // of the gradients; NULL: 1
+  float beta1, new1, beta2, new2;   // new = 1 - beta
+  float rate, decay, root, eps;     // lr / (1 - beta1^k), lr * weight_decay, (1 - beta2^k)^(-1/2)
+  uint32_t key;
+};
+uint32_t adamw_key(uint64_t seed);
+void launch_adamw(const AdamArgs& a, hipStream_t s);
+void launch_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n, bool second, void* x, strata_dtype dt,
+                         hipStream_t s);
+int64_t grad_norm_blocks(int64_t chunks);
+void launch_grad_norm(const ParamRecord* tensors, const int32_t* owner, int64_t chunks, double most, float* norm,
+                      double* partial, hipStream_t s);
 
 // Any supported dtype, head_dim, window and grid, in float32 arithmetic on the
 // float32 matrix instructions; na3d_any_takes: every grid that a device can hold.

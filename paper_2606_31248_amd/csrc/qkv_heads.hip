@@ -52,10 +52,6 @@ __device__ __forceinline__ void rotate(float (&v)[8], const float (&c)[4], const
   }
 }
 
-__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& d) {
-  return d.mul ? __umulhi(n, d.mul) >> d.shift : n;
-}
-
 // A wave's work: `n` heads from h0 of one kind, whose slices of the row start at
 // slice `first`, for the tokens of one tile.
 enum Kind { kQ, kK, kV, kGate };
@@ -490,18 +486,6 @@ __global__ void __launch_bounds__(kSumThreads) weight_sum_kernel(const float* __
     out[(int64_t)blockIdx.y * cols + col] = y;
   else
     (col < cols / 2 ? dwq : dwk)[col < cols / 2 ? col : col - cols / 2] = y;
-}
-
-// n / d for n < 2^31 (d = 1: no multiplier): mul = ceil(2^(31 + l) / d), 2^l >= d, so that n mul / 2^(31 + l)
-// is less than 1/d above n / d.
-static FastDiv fast_div(int64_t d) {
-  FastDiv f;
-  if (d == 1) return f;
-  int l = 1;
-  while (((int64_t)1 << l) < d) ++l;
-  f.mul = (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d);
-  f.shift = l - 1;
-  return f;
 }
 
 static int mode_of(const QkvArgs& a) { return a.codes ? kFromCodes : a.out_codes ? kRowsToCodes : kRows; }

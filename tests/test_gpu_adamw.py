@@ -1,0 +1,373 @@
+"""The norm of the gradients, AdamW over lists of tensors with states in 32 bits and in 8, and the states' values.
+
+m and v, and in 8 bits their codes, are exact: float32 with every product and sum rounded by itself is computed alike
+by numpy.  The weights: m carries 3 roundings of its terms, its product with the rate and the rate itself 2, the root 2,
+its factor and sum with eps 4, the quotient 3: below 2^-19 (32 2^-24) of the update by the terms of m; then decay (3)
+and the last difference, one rounding of the result."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train as T
+from paper_2606_31248_amd import binding as B
+
+from _rows import f64, gen, guarded
+
+pytestmark = pytest.mark.gpu
+
+UPDATE, ONE = 2.0 ** -19, 2.0 ** -24
+HYPER = dict(lr=2e-4, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=1e-2)
+
+
+class Weights:
+    """A list of tensors of these sizes (or shapes), flat states, guards around everything."""
+
+    def __init__(self, sizes, grads="f32", copies=True, eight=False, seed=0, grad_size=1e-3):
+        g = gen(seed + 7)
+        self.checks, self.eight, self.seed = [], eight, seed
+        pick = lambda what, i: what[i % len(what)] if isinstance(what, (list, tuple)) else what  # noqa: E731
+        rand = lambda shape: torch.randn(shape, generator=g)  # noqa: E731
+        self.p = [self.keep((0.02 * rand(s))) for s in sizes]
+        self.g = []
+        for i, p in enumerate(self.p):
+            kind = pick(grads, i)
+            x = rand(tuple(p.shape)) * grad_size * torch.exp(rand((p.numel() // 32 + 1,))).repeat_interleave(32)[:p.numel()].view(p.shape)
+            self.g.append(None if kind is None else self.keep(x.bfloat16() if kind == "bf16" else x))
+        self.copies = [self.keep(p.cpu().bfloat16()) if pick(copies, i) else None for i, p in enumerate(self.p)]
+        self.list = B.make_params(self.p, self.g, self.copies)
+        n = self.list.places
+        self.there = torch.zeros(n, dtype=torch.bool)
+        for at, p in zip(self.list.at, self.p):
+            self.there[at:at + p.numel()] = True
+        size = torch.exp(rand((n // 32,))).repeat_interleave(32) * grad_size * self.there
+        m, v = 0.25 * rand((n,)) * size, size * size * (0.5 + torch.rand((n,), generator=g))
+        if not eight:
+            self.m, self.v, self.m_scales, self.v_scales = self.keep(m), self.keep(v), None, None
+        else:
+            half = np.full(n, 0.5)
+            (mc, ms), (vc, vs) = T.encode(m.numpy(), half, False), T.encode(v.numpy(), half, True)
+            self.m, self.m_scales, self.v, self.v_scales = (self.keep(torch.from_numpy(x)) for x in (mc, ms, vc, vs))
+
+    def keep(self, x):
+        fill = 77 if x.dtype == torch.uint8 else 7.0
+        t, check = guarded(tuple(x.shape), x.dtype, fill)
+        t.copy_(x)
+        self.checks.append(check)
+        return t
+
+    def states(self):
+        """m and v as float64 values, and their scales and codes."""
+        if not self.eight:
+            return f64(self.m), f64(self.v)
+        c = lambda t: t.cpu().numpy()  # noqa: E731
+        return T.decode(c(self.m), c(self.m_scales), False), T.decode(c(self.v), c(self.v_scales), True)
+
+    def flat(self, tensors):
+        out = np.zeros(self.list.places)
+        for at, t in zip(self.list.at, tensors):
+            if t is not None:
+                out[at:at + t.numel()] = f64(t).reshape(-1)
+        return out
+
+    def step(self, k=1000, seed=5, factor=None, **hyper):
+        B.strata_adamw(B.make_adamw_desc(step=k, seed=seed, **dict(HYPER, **hyper)), self.list, self.m, self.v, self.m_scales,
+                       self.v_scales, factor)
+
+    def check_step(self, k=1000, seed=5, factor=None, **hyper):
+        h = dict(HYPER, **hyper)
+        p, g, (m, v) = self.flat(self.p), self.flat(self.g), self.states()
+        raw = [None if t is None else t.cpu().numpy().copy() for t in (self.m, self.v, self.m_scales, self.v_scales)]
+        self.step(k, seed, factor, **hyper)
+        torch.cuda.synchronize()
+        for check in self.checks:
+            check()
+        if factor is not None:
+            g = (np.float32(g) * np.float32(factor.item())).astype(np.float64)
+        moved = np.zeros(self.list.places, bool)            # places of tensors with a gradient, whole groups
+        for at, w, d in zip(self.list.at, self.p, self.g):
+            if d is not None:
+                moved[at:at + (w.numel() + 31) // 32 * 32] = True
+        m32, v32 = T.moments32(g, m, v, h["beta1"], h["beta2"])
+        if self.eight:
+            r = T.random_numbers(seed, np.arange(self.list.places))
+            for i, (got, scales, new, second) in enumerate(((self.m, self.m_scales, m32, False), (self.v, self.v_scales, v32, True))):
+                codes, e = T.encode(new, r[i], second)
+                codes, e = np.where(moved, codes, raw[i]), np.where(moved[::32], e, raw[2 + i])
+                assert np.array_equal(scales.cpu().numpy(), e), "scales of " + "mv"[i]
+                assert np.array_equal(got.cpu().numpy(), codes), "codes of " + "mv"[i]
+        else:
+            assert np.array_equal(self.m.cpu().numpy(), np.where(moved, m32, raw[0]))
+            assert np.array_equal(self.v.cpu().numpy(), np.where(moved, v32, raw[1]))
+        want, _, _ = T.adamw(p, g, m, v, h["lr"], k, h["beta1"], h["beta2"], h["eps"], h["weight_decay"])
+        most = h["lr"] / (1 - h["beta1"] ** k) * (h["beta1"] * np.abs(m) + (1 - h["beta1"]) * np.abs(g)) / \
+            (np.sqrt((h["beta2"] * v + (1 - h["beta2"]) * g * g) / (1 - h["beta2"] ** k)) + h["eps"])
+        want = np.where(moved, want, p)
+        got = self.flat(self.p)
+        assert np.array_equal(np.isnan(got), np.isnan(want))     # of states that hold a NaN
+        worst = np.nanmax(np.abs(got - want) - ONE * np.abs(want) - UPDATE * (most + h["lr"] * h["weight_decay"] * np.abs(p)))
+        assert worst <= 0, f"p off by {worst:.3e} more than its tolerance"
+        for w, c, d in zip(self.p, self.copies, self.g):
+            if c is not None and d is not None:
+                assert np.array_equal(f64(c), f64(w.bfloat16()), equal_nan=True)
+
+
+LISTS = [
+    [1], [31], [32], [33], [4], [5], [128, 128, 128, 128], [1, 2, 3, 4, 5, 6, 7, 8, 9], [2047], [2048], [2049], [1024 * 4 + 3],
+    [(64, 64), (64,), (3, 5, 7), (1,), (2048, 3)], [0, 5, 0, 40], [4096, 100000, 1, 65537],
+]
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("grads", ["f32", "bf16", ["bf16", "f32", "f32"], ["f32", None]])
+@pytest.mark.parametrize("sizes", LISTS, ids=str)
+def test_lists(sizes, grads, eight):
+    w = Weights(sizes, grads, copies=[True, False, True, True], eight=eight)
+    w.check_step()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_first_steps_and_factors(eight):
+    """From states of zeros (8 bits: scales of zeros) over ten steps, each clipped by another factor."""
+    w = Weights([5000, 33, 64], ["f32", "bf16"], eight=eight)
+    for t in (w.m, w.v, w.m_scales, w.v_scales):
+        if t is not None:
+            t.zero_()
+    for k in range(1, 11):
+        w.check_step(k, seed=k, factor=torch.tensor([1.0 / k], device="cuda"))
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("hyper", [dict(beta1=0.0, beta2=0.0), dict(weight_decay=0.0, lr=0.0), dict(eps=1e-3, lr=1.0),
+                                   dict(beta1=0.95, beta2=0.95, k=3), dict(beta2=0.9999999, k=10 ** 9), dict(eps=2.0 ** -100)])
+def test_hyper_parameters(hyper, eight):
+    Weights([3000, 40], "f32", eight=eight, seed=2).check_step(**hyper)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("size", [1e-18, 1e-15, 1e-12, 1e3, 1e12, 1e18])
+def test_sizes_of_gradients(size, eight):
+    """Gradients whose squares come near float32's smallest and largest numbers."""
+    Weights([2000, 70], "f32", eight=eight, seed=3, grad_size=size).check_step(eps=2.0 ** -100)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_weights_of_zero_gradient(eight):
+    """Zero gradients and zero states move nothing but by the decay."""
+    w = Weights([100, 64], "f32", eight=eight)
+    for t in [w.m, w.v] + w.g:
+        t.zero_()
+    if eight:
+        w.m_scales.zero_(), w.v_scales.zero_()
+    w.check_step(1)
+    assert not bool(w.m.any()) and not bool(w.v.any())
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_factor_of_nan_changes_nothing(eight):
+    w = Weights([5000, 33], ["bf16", "f32"], eight=eight)
+    kept = w.p + w.copies + [w.m, w.v] + ([w.m_scales, w.v_scales] if eight else [])
+    was = [t.clone() for t in kept]
+    w.g[0][17] = float("inf")
+    norm = torch.empty(2, device="cuda")
+    ws = torch.empty(B.strata_grad_norm_workspace_size(w.list), dtype=torch.uint8, device="cuda")
+    B.strata_grad_norm(w.list, 1.0, norm, ws)
+    w.step(factor=norm[1:])
+    assert bool(torch.isnan(norm[1])) and float(norm[0]) == float("inf")
+    for a, b in zip(kept, was):
+        assert torch.equal(a, b)
+
+
+def test_gradients_that_are_not_finite_without_a_factor():
+    """Their elements become NaN; in 8 bits the group of 32 does, and stays so.  Other groups are as without them."""
+    w, clean = (Weights([4096, 64], "f32", eight=True) for _ in range(2))
+    w.g[0][40], w.g[1][0] = float("nan"), float("inf")
+    w.step(), clean.step()
+    bad = torch.zeros(w.list.places // 32, dtype=torch.bool, device="cuda")
+    bad[[1, 128]] = True
+    for n in ("m", "v"):
+        got, want = getattr(w, n).view(-1, 32), getattr(clean, n).view(-1, 32)
+        assert torch.equal(got[~bad], want[~bad]) and not bool(got[bad].any())
+        assert bool((getattr(w, n + "_scales")[bad] == 255).all())
+    values = torch.empty(w.list.places, device="cuda")
+    B.strata_adamw_unpack(w.m, w.m_scales, values, second=False)
+    assert torch.equal(torch.isnan(values.view(-1, 32)).all(1), bad) and torch.equal(torch.isnan(values.view(-1, 32)).any(1), bad)
+    assert bool(torch.isnan(w.p[0][40])) and int(torch.isnan(w.p[0]).sum()) == 1
+
+
+def test_eight_bits_follow_32():
+    """200 steps on gradients of a fixed size per weight: the second moment in 8 bits, which moves by less than a
+    code a step, follows the one in 32.  A code is off by up to a step of 1/8; rounded at random it walks, and
+    averages over the 1000 steps that beta2 weighs; over 4096 weights the mean ratio is within a few percent."""
+    n = 4096
+    sizes = torch.exp(0.5 * torch.randn(n, generator=gen(1))).cuda()
+    a, b = Weights([n], "f32", eight=True), Weights([n], "f32")
+    for w in (a, b):
+        for t in (w.m, w.v, w.m_scales, w.v_scales):
+            if t is not None:
+                t.zero_()
+    for k in range(1, 201):
+        g = torch.randn(n, generator=gen(1000 + k)).cuda() * sizes * 1e-3
+        for w in (a, b):
+            w.g[0].copy_(g)
+            w.step(k, seed=k, weight_decay=0.0)
+    m, v = a.states()
+    ratio = v / f64(b.v)
+    # a walk of 200 roundings, each of variance at most (value/8)^2 p (1 - p) with p the share of a step that the
+    # value moves (from zero: 1/k at step k): below 200 / 64 2^-3 summed, a deviation of 0.3 each, 0.3 / 64 in the mean
+    assert abs(ratio.mean() - 1) < 5 * 0.3 / 64
+    assert np.linalg.norm(m - f64(b.m)) < 0.1 * np.linalg.norm(f64(b.m))
+
+
+@pytest.mark.parametrize("second", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_unpack(second, dtype):
+    """Every code under every scale that states have, and lengths that end inside a group and a lane's piece."""
+    e = [0, 1] + list(range(T.UNIT[second] + 1, 256))
+    codes = np.tile(np.arange(256, dtype=np.uint8), len(e))
+    scales = np.repeat(np.array(e, np.uint8), 8)
+    for n in (1, 7, 8, 9, 31, 32, 33, 2047, 2048, 2049, codes.size):
+        c, s = torch.from_numpy(codes[:n]).cuda(), torch.from_numpy(scales[:(n + 31) // 32]).cuda()
+        x, check = guarded((n,), dtype)
+        B.strata_adamw_unpack(c, s, x, second)
+        check()
+        want = T.decode(codes[:n], scales[:(n + 31) // 32], second)
+        got = f64(x)
+        assert np.array_equal(got, want, equal_nan=True)
+
+
+# ---- the norm of the gradients ---------------------------------------------------------
+
+def grad_norm(w, most):
+    norm, check = guarded((2,), torch.float32)
+    ws, ws_check = guarded((B.strata_grad_norm_workspace_size(w.list),), torch.uint8, 77)
+    B.strata_grad_norm(w.list, most, norm, ws)
+    torch.cuda.synchronize()
+    check(), ws_check()
+    return norm.cpu().double().numpy()
+
+
+@pytest.mark.parametrize("grads", ["f32", "bf16", ["bf16", "f32"], ["f32", None]])
+@pytest.mark.parametrize("sizes", LISTS + [[2048] * 5000], ids=lambda s: str(s)[:30])
+def test_grad_norm(sizes, grads):
+    w = Weights(sizes, grads, copies=False)
+    n = float(np.sqrt((w.flat(w.g) ** 2).sum()))
+    for most in (n / 3 + 1e-30, n * 2 + 1e-30, float("inf"), 1e-20):
+        got = grad_norm(w, most)
+        factor = 1.0 if n <= most else most / n
+        # float64 sums of at most 2^24 squares, rounded once to float32
+        assert abs(got[0] - n) <= ONE * n * 1.001 and abs(got[1] - factor) <= ONE * factor * 1.001
+
+
+def test_grad_norm_without_gradients():
+    w = Weights([100, 7], [None], copies=False)
+    assert grad_norm(w, 1.0).tolist() == [0.0, 1.0]
+    was = [p.clone() for p in w.p]
+    w.step()
+    assert all(torch.equal(a, b) for a, b in zip(w.p, was))
+
+
+def test_grad_norm_ranges():
+    """Squares beyond float32's range on both sides; infinities and NaN."""
+    w = Weights([3000, 10], "f32", copies=False)
+    for value in (1e-30, 1e30, 3e38):
+        for g in w.g:
+            g.fill_(value)
+        n = float(np.float32(value)) * 3010 ** 0.5
+        got = grad_norm(w, 1.0)
+        if n < 3.4e38:
+            assert abs(got[0] - n) <= ONE * n * 1.001
+        else:
+            assert got[0] == float("inf")
+        f = min(1.0, 1.0 / n)
+        assert abs(got[1] - f) <= max(ONE * f * 1.001, 2.0 ** -150)
+    for value in (float("inf"), float("nan"), float("-inf")):
+        w.g[0].fill_(1.0)
+        w.g[0][2999] = value
+        got = grad_norm(w, 1.0)
+        assert np.isnan(got[1]) and (np.isnan(got[0]) or got[0] == float("inf"))
+
+
+# ---- together ------------------------------------------------------------------------
+
+def test_streams_and_replays():
+    """Norm, clipping and AdamW on another stream, and captured: a replay repeats the call on what is there then."""
+    def update(w, norm, ws, stream=None):
+        B.strata_grad_norm(w.list, 0.01, norm, ws, stream=stream)
+        B.strata_adamw(B.make_adamw_desc(step=7, seed=3, **HYPER), w.list, w.m, w.v, w.m_scales, w.v_scales, norm[1:], stream=stream)
+    for eight in (False, True):
+        a, b, c = (Weights([3000, 100, 2049], ["bf16", "f32"], eight=eight) for _ in range(3))
+        new = lambda w: (torch.empty(2, device="cuda"),  # noqa: E731
+                         torch.empty(B.strata_grad_norm_workspace_size(w.list), dtype=torch.uint8, device="cuda"))
+        s = torch.cuda.Stream()
+        na, nb, nc = new(a), new(b), new(c)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            update(c, *nc)
+        for k in range(4):
+            update(a, *na)
+            update(b, *nb, stream=s)
+            graph.replay()
+            torch.cuda.synchronize()
+            for other in (b, c):
+                for x, y in zip(a.p + a.copies + [a.m, a.v], other.p + other.copies + [other.m, other.v]):
+                    assert torch.equal(x, y)
+            for i, g in enumerate(a.g):
+                for w in (a, b, c):
+                    w.g[i].copy_(torch.randn(tuple(g.shape), generator=gen(50 + k)) * 1e-3)
+
+
+def test_beyond_32_bit_offsets():
+    """32-bit states of two tensors of 2^31 + 100 weights each: the second lies behind place 2^31."""
+    n = (1 << 31) + 100
+    p = [torch.zeros(n, device="cuda") for _ in range(2)]
+    g = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    w = B.make_params(p, g)
+    m, v = (torch.zeros(w.places, device="cuda") for _ in range(2))
+    at = [0, 1 << 30, (1 << 31) - 1, 1 << 31, n - 1]
+    for t in g:
+        t[at] = torch.tensor([1.0, -2.0, 3.0, -4.0, 5.0], device="cuda").bfloat16()
+    norm, ws = torch.empty(2, device="cuda"), torch.empty(B.strata_grad_norm_workspace_size(w), dtype=torch.uint8, device="cuda")
+    B.strata_grad_norm(w, float("inf"), norm, ws)
+    B.strata_adamw(B.make_adamw_desc(1e-3, 1), w, m, v)
+    assert abs(float(norm[0]) - 110 ** 0.5) < 2.0 ** -20 and float(norm[1]) == 1.0
+    for i, t in enumerate(p):
+        # the first step is lr times the sign, to the digits of eps against the gradient
+        assert np.allclose(f64(t[at]), [-1e-3, 1e-3, -1e-3, 1e-3, -1e-3], rtol=1e-5)
+        assert int((t != 0).sum()) == 5
+        assert np.allclose(f64(m[w.at[i]:][at]), 0.1 * np.array([1, -2, 3, -4, 5]), rtol=1e-6)
+    assert int((m != 0).sum()) == 10 and int((v != 0).sum()) == 10
+    del p, g, m, v
+    torch.cuda.empty_cache()
+
+
+def test_refusals():
+    w = Weights([64, 33], "f32")
+    p, g, c = w.p, w.g, w.copies
+    for a in (([p[0].cpu()], [g[0]], None), ([p[0]], [g[0].cpu()], None), ([p[0].double()], [g[0]], None),
+              ([p[0]], [g[0].half()], None), ([p[0]], [g[0][:63]], None), ([p[0]], [g[0]], [c[0].float()]),
+              ([p[0]], [g[0]], [c[0][:5]]), ([torch.zeros(8, 8, device="cuda").t()], [torch.zeros(8, 8, device="cuda")], None),
+              ([5], [g[0]], None), ([None], [g[0]], None)):
+        with pytest.raises(ValueError):
+            B.make_params(*a)
+    with pytest.raises(B.StrataError, match="twice"):
+        B.make_params([p[0], p[0]], [g[0], g[0]])
+    with pytest.raises(B.StrataError, match="aligned"):
+        B.make_params([p[0][1:33]], [g[0][:32]])
+    d = B.make_adamw_desc(1e-3, 1)
+    u8 = lambda n: torch.zeros(n, dtype=torch.uint8, device="cuda")  # noqa: E731
+    for m, v, ms, vs, f in ((w.m[:97], w.v, None, None, None), (w.m, w.v.double(), None, None, None), (w.m.cpu(), w.v, None, None, None),
+                            (w.m, w.v, u8(4), u8(4), None), (u8(128), u8(128), None, None, None), (u8(128), u8(128), u8(4), None, None),
+                            (u8(128), u8(128), u8(4), u8(5), None), (w.m, w.v, None, None, torch.ones(2, device="cuda")),
+                            (w.m, w.v, None, None, torch.ones(1)), (w.m, None, None, None, None)):
+        with pytest.raises(ValueError):
+            B.strata_adamw(d, w.list, m, v, ms, vs, f)
+    with pytest.raises(ValueError):
+        B.strata_grad_norm(w.list, 1.0, torch.empty(3, device="cuda"), u8(4096))
+    with pytest.raises(B.StrataError):
+        B.strata_grad_norm(w.list, 1.0, torch.empty(2, device="cuda"), None)
+    for a in ((u8(32), u8(1), torch.empty(33, device="cuda")), (u8(33), u8(1), torch.empty(33, device="cuda")),
+              (u8(32).view(torch.int8), u8(1), torch.empty(32, device="cuda")), (u8(32), u8(1), torch.empty(32)),
+              (u8(32), u8(1), torch.empty(32, device="cuda", dtype=torch.float16))):
+        with pytest.raises(ValueError):
+            B.strata_adamw_unpack(*a, second=False)

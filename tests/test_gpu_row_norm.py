@@ -1,0 +1,339 @@
+"""The residual stream's addition and RMS norm (strata_residual_norm) and its gradients against the oracle in 64 bits.
+
+Tolerances.  sum: one rounding to its type, and one in float32 relative to the terms.  The oracle then takes the sum
+that came back.  y: the mean of up to 8192 squares is 16 additions in a lane, a tree of 6 and 8 waves' (30 2^-24),
+half of that in its root, the reciprocal root 2, three more products: below 2^-19 (32 2^-24) of the terms, and one
+rounding to the type.  The gradient of the rows: u and n are within 20 2^-24, their products' mean, added like the
+squares, within 40 + 32, n times it 92, the last sums 2: below 2^-17 (128 2^-24) of the terms.  The vectors'
+gradients add these over rows, at most 256 in a row: below 2^-15 (512 2^-24) of the terms."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rows as R
+from oracle import train as T
+from paper_2606_31248_amd import binding as B
+
+from _rows import ARITH, HALF_STEP, TYPE, f64, gen, guarded, normal
+
+pytestmark = pytest.mark.gpu
+
+ROW_GRAD, VECTOR_GRAD, ONE = 2.0 ** -17, 2.0 ** -15, 2.0 ** -24
+EPS = 1e-6
+
+
+class Norm:
+    """Inputs and guarded outputs of one case: `has` of x, gate, scale, shift, dsum, codes."""
+
+    def __init__(self, dtype, groups, group_rows, width, has="x gate scale shift dsum", seed=0, eps=EPS, mult=1.0):
+        g = gen(seed + 31 * width + groups)
+        has = set(has.split())
+        rows = (groups * group_rows, width)
+        self.dtype, self.groups, self.group_rows, self.width, self.eps, self.rows = dtype, groups, group_rows, width, eps, rows
+        self.res = normal(rows, dtype, g, 2.0 * mult) * torch.exp(0.5 * torch.randn(width, generator=g)).to(TYPE[dtype]).cuda()
+        self.x = normal(rows, dtype, g, mult) if "x" in has else None
+        vec = lambda name, mean: (mean + 0.3 * torch.randn((groups, width), generator=g)).cuda() if name in has else None  # noqa: E731
+        self.gate, self.scale, self.shift = vec("gate", 0.5), vec("scale", 1.0), vec("shift", 0.0)
+        self.dy = normal(rows, dtype, g)
+        self.dsum = normal(rows, dtype, g) if "dsum" in has else None
+        self.eight = "codes" in has
+        self.desc = B.make_norm_desc(self.res, group_rows, eps)
+        self.checks = []
+
+    def new(self, shape, dtype, fill=7.0):
+        t, check = guarded(shape, dtype, fill)
+        self.checks.append(check)
+        return t
+
+    def like(self, t, dtype=None):
+        return None if t is None else self.new(tuple(t.shape), dtype or t.dtype)
+
+    def forward(self, y=True):
+        codes = self.new(self.rows, torch.int8, 77) if self.eight else None
+        scales = self.new((self.rows[0], self.width // 32), torch.uint8, 77) if self.eight else None
+        out = dict(sum=self.like(self.x), y=self.like(self.res) if y else None, codes=codes, scales=scales)
+        B.strata_residual_norm(self.desc, self.x, self.gate, self.res, self.scale, self.shift, out["sum"], out["y"], codes, scales)
+        return out
+
+    def backward(self, total, shift=True):
+        gated = self.gate is not None
+        out = dict(dres=self.like(self.res), dx=self.like(self.res) if gated else None, dgate=self.like(self.gate),
+                   dscale=self.like(self.scale), dshift=self.new((self.groups, self.width), torch.float32) if shift else None)
+        ws = self.new((B.strata_residual_norm_bwd_workspace_size(self.desc),), torch.uint8, 77)
+        B.strata_residual_norm_bwd(self.desc, total, self.x if gated else None, self.gate, self.scale, self.dy, self.dsum,
+                                   out["dres"], out["dx"], out["dgate"], out["dscale"], out["dshift"], ws)
+        return out
+
+    def guards(self):
+        torch.cuda.synchronize()
+        for check in self.checks:
+            check()
+
+    def cube(self, t):
+        return None if t is None else f64(t).reshape(self.groups, self.group_rows, self.width)
+
+
+def within(got, want, tol, what):
+    worst = np.max(np.abs(got - want) - tol)
+    assert worst <= 0, f"{what}: off by {worst:.3e} more than its tolerance"
+
+
+def check_forward(c, out):
+    half = HALF_STEP[c.dtype]
+    res, x, gate, scale, shift = (c.cube(c.res), c.cube(c.x), f64(c.gate), f64(c.scale), f64(c.shift))
+    total = res
+    if x is not None:
+        want = T.add(res, x, gate)
+        total = c.cube(out["sum"])
+        within(total, want, half * np.abs(want) + ONE * (np.abs(res) + np.abs(want - res)), "sum")
+    y, n, _ = T.norm(total, scale, shift, c.eps)
+    terms = np.abs(n if scale is None else n * scale[:, None]) + (0 if shift is None else np.abs(shift[:, None]))
+    if out["y"] is not None:
+        within(c.cube(out["y"]), y, half * (np.abs(y) + ARITH * terms) + ARITH * terms, "y")
+    return total
+
+
+def check_backward(c, total, out):
+    half = HALF_STEP[c.dtype]
+    want = T.norm_backward(total, c.cube(c.dy), c.cube(c.dsum), c.cube(c.x) if c.gate is not None else None, f64(c.gate),
+                           f64(c.scale), c.eps)
+    for name, got in out.items():
+        if got is None:
+            continue
+        mag = want["mag_" + name]
+        if name in ("dres", "dx"):
+            within(c.cube(got), want[name], half * np.abs(want[name]) + (1 + half) * ROW_GRAD * mag, name)
+        else:
+            within(f64(got), want[name], VECTOR_GRAD * mag, name)
+
+
+def check(c, shift=True):
+    out = c.forward()
+    total = check_forward(c, out)
+    grads = c.backward(c.res if c.x is None else out["sum"], shift)
+    check_backward(c, total, grads)
+    c.guards()
+    if c.eight:
+        codes, scales = R.encode(f64(out["y"]))
+        assert np.array_equal(out["codes"].cpu().numpy().reshape(-1), codes)
+        assert np.array_equal(out["scales"].cpu().numpy().reshape(-1), scales)
+    return out, grads
+
+
+# widths on both sides of every team of lanes, of one and two pieces a lane, of a wave and of 2 to 8 waves
+WIDTHS = [1, 2, 7, 8, 9, 31, 32, 33, 40, 63, 64, 65, 127, 128, 129, 203, 256, 257, 509, 512, 513, 520, 768, 1000, 1023, 1024,
+          1025, 1032, 1536, 2047, 2048, 2049, 4096, 5000, 8185, 8191, 8192]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_widths(width, dtype):
+    check(Norm(dtype, 2, 9, width, "x gate scale shift dsum" + (" codes" if width % 32 == 0 else "")))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("groups,group_rows", [(1, 1), (1, 2), (1, 3), (1, 17), (5, 1), (70, 1), (3, 2), (2, 37), (64, 3),
+                                               (1, 500), (7, 129), (1030, 2)])
+@pytest.mark.parametrize("width", [8, 24, 100, 128, 640])
+def test_rows_and_groups(groups, group_rows, width, dtype):
+    check(Norm(dtype, groups, group_rows, width))
+
+
+HAS = [" ".join(n for n, on in zip(("x", "gate", "scale", "shift", "dsum"), bits) if on)
+       for bits in itertools.product((0, 1), repeat=5) if bits[0] or not bits[1]]
+
+
+@pytest.mark.parametrize("has", HAS)
+def test_what_is_left_out(has):
+    """Every set of x, gate, scale, shift and dsum; the shift's gradient is asked for with or without a shift."""
+    for dtype, width in (("bf16", 96), ("f32", 130), ("bf16", 1100)):
+        check(Norm(dtype, 3, 5, width, has), shift="dsum" in has)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(40000, 128), (9000, 1024), (5000, 1536), (70000, 24)])
+def test_many_rows(rows, width, dtype):
+    """Teams that take several rows in the forward and, over many blocks, in the backward.  Sums over more rows than
+    the tolerance counts in a row are still added in at most 256 steps: spans of rows, then blocks."""
+    check(Norm(dtype, 2, rows // 2, width))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_alone(dtype):
+    """Without y the codes are the same, and so is the sum."""
+    for width, groups in ((32, 3), (64, 1), (96, 2), (1024, 2), (2080, 1)):
+        c = Norm(dtype, groups, 11, width, "x gate scale shift codes")
+        both, alone = c.forward(), c.forward(y=False)
+        for n in ("sum", "codes", "scales"):
+            assert torch.equal(both[n], alone[n])
+        back = torch.empty_like(c.res)
+        B.strata_ckpt_unpack(alone["codes"], alone["scales"], back)
+        codes, scales = torch.empty_like(alone["codes"]), torch.empty_like(alone["scales"])
+        B.strata_ckpt_pack(both["y"], codes, scales)
+        assert torch.equal(codes, alone["codes"]) and torch.equal(scales, alone["scales"])
+        c.guards()
+
+
+def test_in_place():
+    """sum into res or x, dres into dsum or dy, dx into x: as elsewhere, bit for bit."""
+    for dtype, width in (("bf16", 136), ("f32", 203), ("bf16", 3000), ("bf16", 1024)):
+        c = Norm(dtype, 2, 700, width)
+        out = c.forward()
+        grads = c.backward(out["sum"])
+        for name in ("res", "x"):
+            d = Norm(dtype, 2, 700, width)
+            y = torch.empty_like(d.res)
+            B.strata_residual_norm(d.desc, d.x, d.gate, d.res, d.scale, d.shift, getattr(d, name), y)
+            assert torch.equal(getattr(d, name), out["sum"]) and torch.equal(y, out["y"])
+        for name in ("dsum", "dy"):
+            d = Norm(dtype, 2, 700, width)
+            ws = torch.empty(B.strata_residual_norm_bwd_workspace_size(d.desc), dtype=torch.uint8, device="cuda")
+            v = [torch.empty_like(d.gate) for _ in range(3)]
+            B.strata_residual_norm_bwd(d.desc, out["sum"], d.x, d.gate, d.scale, d.dy, d.dsum, getattr(d, name), d.x, *v, ws)
+            assert torch.equal(getattr(d, name), grads["dres"]) and torch.equal(d.x, grads["dx"])
+            for got, n in zip(v, ("dgate", "dscale", "dshift")):
+                assert torch.equal(got, grads[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ranges_of_the_norm(dtype):
+    """Rows from 2^-60 to 2^56 with an eps that does not matter, rows of zeros, one value among zeros."""
+    t = TYPE[dtype]
+    c = Norm(dtype, 1, 120, 72, "scale", eps=2.0 ** -125)
+    for i in range(117):
+        c.res[i] = (normal((72,), dtype, gen(i)).double() * 2.0 ** (i - 60)).to(t)
+        c.dy[i] = (normal((72,), dtype, gen(500 + i)).double() * 2.0 ** -(i // 2)).to(t)
+    c.res[117] = 0
+    c.res[118] = 0
+    c.res[118, 5] = 3.0
+    c.res[119] = 1.0
+    check(c)
+
+
+def test_rows_that_are_not_finite_stay_alone():
+    """An infinity or a NaN makes its row NaN (an infinite row: 0 and NaN), its 8-bit groups too, and no other row."""
+    c = Norm("bf16", 1, 40, 64, "x scale codes")
+    clean = c.forward()
+    c.x[3, 5], c.res[17, 0], c.res[30, 63] = float("nan"), float("inf"), float("-inf")
+    out = c.forward()
+    bad = torch.zeros(40, dtype=torch.bool, device="cuda")
+    bad[[3, 17, 30]] = True
+    for n in ("sum", "y", "codes", "scales"):
+        assert torch.equal(out[n][~bad], clean[n][~bad])
+    assert not bool(torch.isfinite(out["y"][bad]).all(1).any())
+    held = torch.empty_like(out["y"])
+    B.strata_ckpt_unpack(out["codes"], out["scales"], held)
+    groups = torch.isfinite(out["y"].view(-1, 32)).all(1)
+    assert bool(torch.isnan(held.view(-1, 32)[~groups]).all()) and bool(torch.isfinite(held.view(-1, 32)[groups]).all())
+
+
+def test_gradient_by_differences():
+    """float32, a loss in 64 bits of the kernel's own forward: central differences of 2^-7 in directions of unit size
+    are off by their third order (below 2^-14 of the value here) and by the forward's rounding over 2^-7."""
+    c = Norm("f32", 2, 6, 40)
+    out = c.forward()
+    grads = c.backward(out["sum"])
+
+    def loss():
+        o = c.forward()
+        return float((o["y"].double() * c.dy.double()).sum() + (o["sum"].double() * c.dsum.double()).sum())
+    for name, grad in (("res", "dres"), ("x", "dx"), ("gate", "dgate"), ("scale", "dscale"), ("shift", "dshift")):
+        t, keep = getattr(c, name), getattr(c, name).clone()
+        for seed in range(3):
+            d = normal(tuple(t.shape), "f32", gen(900 + seed))
+            h = 2.0 ** -7 / float(d.norm())
+            diff = []
+            for f in (h, -h):
+                t.copy_(keep + f * d)
+                diff.append(loss())
+            t.copy_(keep)
+            want = float((grads[grad].double() * d.double()).sum())
+            # outputs of order 4 with 480 rounding errors of 2^-24 relative, twice, over 2 h
+            noise = 4 * 2.0 ** -24 * 480 ** 0.5 * float(c.dy.norm()) / 480 ** 0.5 * 8 / h
+            assert abs((diff[0] - diff[1]) / (2 * h) - want) <= 2.0 ** -12 * float(grads[grad].norm() * d.norm()) + noise
+
+
+def test_streams_and_replays():
+    """On another stream, and forward and backward captured together, replayed on other inputs between eager calls."""
+    c = Norm("bf16", 3, 50, 192, "x gate scale shift dsum codes")
+    out = c.forward()
+    grads = c.backward(out["sum"])
+    s = torch.cuda.Stream()
+    other = [torch.empty_like(out[n]) for n in ("sum", "y")]
+    torch.cuda.synchronize()
+    B.strata_residual_norm(c.desc, c.x, c.gate, c.res, c.scale, c.shift, *other, stream=s)
+    s.synchronize()
+    assert torch.equal(other[0], out["sum"]) and torch.equal(other[1], out["y"])
+    new = {n: torch.empty_like(t) for n, t in {**out, **grads}.items()}
+    ws = torch.empty(B.strata_residual_norm_bwd_workspace_size(c.desc), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.strata_residual_norm(c.desc, c.x, c.gate, c.res, c.scale, c.shift, *(new[n] for n in out))
+        B.strata_residual_norm_bwd(c.desc, new["sum"], c.x, c.gate, c.scale, c.dy, c.dsum, *(new[n] for n in grads), ws)
+    for seed in (1, 2, 3):
+        for name in ("res", "x", "dy", "dsum"):
+            getattr(c, name).copy_(normal(c.rows, "bf16", gen(seed)))
+        want = c.forward()
+        want = {**want, **c.backward(want["sum"])}
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in want:
+            assert torch.equal(new[n], want[n]), n
+
+
+def test_beyond_32_bit_offsets():
+    """Rows on both sides of element 2^31 and 2^32 (bf16, width 8192), and their gradients."""
+    width, rows = 8192, (1 << 19) + 40
+    t = dict(dtype=torch.bfloat16, device="cuda")
+    res, y, dy = (torch.empty((rows, width), **t) for _ in range(3))
+    res.fill_(1.0)
+    dy.fill_(0.0)
+    places = [0, 1, (1 << 18) - 1, 1 << 18, (1 << 19) - 1, 1 << 19, rows - 1]
+    for i, at in enumerate(places):
+        res[at], dy[at] = normal((width,), "bf16", gen(i)), normal((width,), "bf16", gen(50 + i))
+    scale = (1 + 0.3 * torch.randn((1, width), generator=gen(9))).cuda()
+    d = B.make_norm_desc(res, eps=EPS)
+    B.strata_residual_norm(d, None, None, res, scale, None, None, y)
+    want, n, _ = T.norm(f64(res[places])[None], f64(scale), eps=EPS)
+    within(f64(y[places]), want[0], HALF_STEP["bf16"] * np.abs(want[0]) * (1 + ARITH) + 2 * ARITH * np.abs(want[0]), "y")
+    others = torch.ones(rows, dtype=torch.bool, device="cuda")
+    others[places] = False
+    one = y[2]
+    assert bool((y[others] == one).all())
+    dscale, ws = torch.empty_like(scale), torch.empty(B.strata_residual_norm_bwd_workspace_size(d), dtype=torch.uint8, device="cuda")
+    B.strata_residual_norm_bwd(d, res, None, None, scale, dy, None, y, dscale=dscale, workspace=ws)
+    want = T.norm_backward(f64(res[places])[None], f64(dy[places])[None], scale=f64(scale), eps=EPS)
+    within(f64(y[places]), want["dres"][0], HALF_STEP["bf16"] * np.abs(want["dres"][0]) + 2 * ROW_GRAD * want["mag_dres"][0], "dres")
+    within(f64(dscale), want["dscale"], VECTOR_GRAD * want["mag_dscale"], "dscale")   # the other rows add exact zeros
+    assert bool((y[others] == 0).all())
+    del res, y, dy
+    torch.cuda.empty_cache()
+
+
+def test_refusals():
+    c = Norm("bf16", 2, 4, 64, "x gate scale shift dsum codes")
+    o = c.forward()
+    good = dict(x=c.x, gate=c.gate, res=c.res, scale=c.scale, shift=c.shift, sum=o["sum"], y=o["y"], codes=o["codes"],
+                scales=o["scales"])
+    wide = torch.empty((8, 128), dtype=torch.bfloat16, device="cuda")
+    for kw in (dict(x=c.x.float()), dict(x=c.x[:7]), dict(x=c.x.view(16, 32)), dict(res=wide[:, ::2]), dict(res=c.res.cpu()),
+               dict(gate=c.gate[0]), dict(gate=c.gate.view(-1)), dict(scale=c.scale.double()), dict(shift=c.shift[:, :63]),
+               dict(sum=o["sum"].float()), dict(y=o["y"].float()), dict(y=o["y"].cpu()), dict(codes=o["codes"].view(torch.uint8)),
+               dict(codes=o["codes"][:7]), dict(scales=o["scales"][:7]), dict(scales=o["scales"].view(torch.int8)),
+               dict(res=None), dict(res=5)):
+        with pytest.raises(ValueError):
+            B.strata_residual_norm(c.desc, **dict(good, **kw))
+    g = c.backward(o["sum"])
+    ws = torch.empty(B.strata_residual_norm_bwd_workspace_size(c.desc), dtype=torch.uint8, device="cuda")
+    good = dict(sum=o["sum"], x=c.x, gate=c.gate, scale=c.scale, dy=c.dy, dsum=c.dsum, workspace=ws, **g)
+    for kw in (dict(sum=c.res.float()), dict(dy=c.dy[:7]), dict(dsum=c.dsum.float()), dict(dres=g["dres"].cpu()),
+               dict(dgate=g["dgate"][:1]), dict(dscale=g["dscale"].bfloat16()), dict(workspace=ws.cpu()), dict(dx=g["dx"][:3])):
+        with pytest.raises(ValueError):
+            B.strata_residual_norm_bwd(c.desc, **dict(good, **kw))
+    single = Norm("bf16", 1, 4, 64, "scale")
+    y = torch.empty_like(single.res)
+    B.strata_residual_norm(single.desc, None, None, single.res, single.scale[0], None, None, y)   # one group: [width] too
+    assert torch.equal(y, single.forward()["y"])
+    c.guards()
