@@ -377,7 +377,7 @@ static strata_status check_norm(const strata_norm_desc* d, NormArgs* a) {
     return set_error(STRATA_ERR_UNSUPPORTED, "norm: width %d not supported (at most %d)", d->width, kMaxNormWidth);
   REQUIRE(d->rows * d->width < kMaxElems, "norm: tensor too large");
   a->rows = d->rows, a->group_rows = d->group_rows, a->groups = d->rows / d->group_rows;
-  a->width = d->width, a->eps = d->eps;
+  a->width = d->width, a->eps = d->eps, a->inverse = 1.f / d->width;
   return STRATA_OK;
 }
 

@@ -100,10 +100,8 @@ struct NormArgs {
   float* partial = nullptr;         // [vectors with a gradient][groups * chunks][width]
   int64_t rows = 0, group_rows = 0, groups = 0;
   int width = 0;
-  float eps = 0.f;
-  // the launch: forward, rows that a team takes; backward, blocks and rows of a block of one group
-  int steps = 1;
-  int64_t chunks = 0, span = 0;
+  float eps = 0.f, inverse = 0.f;   // 1 / width
+  int64_t blocks = 0, chunks = 0;   // of the forward, and of a group in the backward
   FastDiv by_group;
 };
 void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s);

@@ -16,9 +16,53 @@ using namespace ckpt8;
 
 constexpr int kWaves = 4;               // of a block, where a row fits a wave
 constexpr int kMaxWaves = 8;            // of a row: 8192 channels
-constexpr int kSpan = 8;                // channels of a lane's piece
 
-// 8 elements from any address of the type's alignment, whole or the first `n` of them.
+// A lane's channels of a piece: 4 and 4, side by side in bf16 (16 bytes), in float32 4 in
+// each half of the piece, so that both are 16 bytes beside the neighbours'.  In the last
+// piece of a row less of them may be there.
+struct Part {
+  int lo, hi;  // of the first and the second 4
+};
+
+// How a row lies: kLines, whole cache lines that are streamed; kWhole, a multiple of 8
+// channels, so that 4 are there or none; kRagged, of any width.
+enum Lie { kLines, kWhole, kRagged };
+
+// Four elements, 16 bytes of float32, from any address of the type's alignment.  Of a ragged
+// row the lanes at its end load what follows too, which is the next row but behind the last;
+// `keep` clears that where it would count, not here, so that the load stays in flight.
+typedef u32x4 __attribute__((aligned(4))) float_quad;
+template <int LIE>
+__device__ __forceinline__ u32x4 load_quad(const float* p, int n, bool inside) {
+  u32x4 v = {};
+  if (LIE == kLines) {
+    if (n) v = load16(p);
+  } else if (LIE == kWhole) {
+    if (n) v = *reinterpret_cast<const u32x4*>(p);
+  } else if (inside) {
+    v = *reinterpret_cast<const float_quad*>(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) v[j] = __float_as_uint(p[j]);
+  }
+  return v;
+}
+template <int LIE>
+__device__ __forceinline__ void store_quad(float* p, int n, u32x4 v) {
+  if (n == 4) {
+    if (LIE == kLines)
+      store16(p, v);
+    else
+      *reinterpret_cast<float_quad*>(p) = v;
+  } else if (LIE == kRagged) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = __uint_as_float(v[j]);
+  }
+}
+
+// A lane's 8 elements of a piece as they lie in memory, at `at` of `size` and `gap` behind.
 template <bool BF16>
 struct Piece;
 template <>
@@ -26,93 +70,99 @@ struct Piece<true> {
   typedef u32x4 __attribute__((aligned(2))) any;
   u32x4 a;
   __device__ __forceinline__ void clear() { a = u32x4{}; }
-  __device__ __forceinline__ void load(const void* p) { a = *static_cast<const any*>(p); }
-  __device__ __forceinline__ void load_part(const void* p, int n) {
-    const uint16_t* q = static_cast<const uint16_t*>(p);
-    a = u32x4{};
+  template <int LIE>
+  __device__ __forceinline__ void load(const void* base, int64_t at, int, Part n, int64_t size) {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+    const int many = n.lo + n.hi;
+    clear();
+    if (LIE == kLines) {
+      if (many) a = load16(p);
+    } else if (LIE == kWhole) {
+      if (many) a = *reinterpret_cast<const u32x4*>(p);
+    } else if (at + 8 <= size) {
+      a = *reinterpret_cast<const any*>(p);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) a[j >> 1] |= (uint32_t)q[j] << (16 * (j & 1));
+      for (int j = 0; j < 8; ++j)
+        if (j < many) a[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    }
+  }
+  template <int LIE>
+  __device__ __forceinline__ void keep(Part n) {
+    const int many = n.lo + n.hi;
+    if (LIE != kRagged) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] &= many > 2 * j + 1 ? ~0u : many > 2 * j ? 0xFFFFu : 0u;
   }
   __device__ __forceinline__ void get(float (&v)[8]) const { widen(a, v); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = mfma::pack2(v[2 * i], v[2 * i + 1]);
   }
-  __device__ __forceinline__ void store(void* p) const { *static_cast<any*>(p) = a; }
-  __device__ __forceinline__ void store_part(void* p, int n) const {
-    uint16_t* q = static_cast<uint16_t*>(p);
+  template <int LIE>
+  __device__ __forceinline__ void store(void* base, int64_t at, int, Part n) const {
+    uint16_t* p = static_cast<uint16_t*>(base) + at;
+    const int many = n.lo + n.hi;
+    if (many == 8) {
+      if (LIE == kLines)
+        store16(p, a);
+      else
+        *reinterpret_cast<any*>(p) = a;
+    } else if (LIE == kRagged) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) q[j] = (uint16_t)(a[j >> 1] >> (16 * (j & 1)));
+      for (int j = 0; j < 8; ++j)
+        if (j < many) p[j] = (uint16_t)(a[j >> 1] >> (16 * (j & 1)));
+    }
   }
 };
 template <>
 struct Piece<false> {
-  typedef u32x4 __attribute__((aligned(4))) any;
   u32x4 a, b;
   __device__ __forceinline__ void clear() { a = b = u32x4{}; }
-  __device__ __forceinline__ void load(const void* p) { a = static_cast<const any*>(p)[0], b = static_cast<const any*>(p)[1]; }
-  __device__ __forceinline__ void load_part(const void* p, int n) {
-    const uint32_t* q = static_cast<const uint32_t*>(p);
-    clear();
+  template <int LIE>
+  __device__ __forceinline__ void load(const void* base, int64_t at, int gap, Part n, int64_t size) {
+    const float* p = static_cast<const float*>(base) + at;
+    a = load_quad<LIE>(p, n.lo, at + 4 <= size);
+    b = load_quad<LIE>(p + gap, n.hi, at + gap + 4 <= size);
+  }
+  template <int LIE>
+  __device__ __forceinline__ void keep(Part n) {
+    if (LIE != kRagged) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j < n) a[j] = q[j];
-      if (4 + j < n) b[j] = q[4 + j];
-    }
+    for (int j = 0; j < 4; ++j) a[j] = n.lo > j ? a[j] : 0u, b[j] = n.hi > j ? b[j] : 0u;
   }
   __device__ __forceinline__ void get(float (&v)[8]) const { as_floats(a, b, v); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]), b[i] = __float_as_uint(v[4 + i]);
   }
-  __device__ __forceinline__ void store(void* p) const { static_cast<any*>(p)[0] = a, static_cast<any*>(p)[1] = b; }
-  __device__ __forceinline__ void store_part(void* p, int n) const {
-    uint32_t* q = static_cast<uint32_t*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j < n) q[j] = a[j];
-      if (4 + j < n) q[4 + j] = b[j];
-    }
+  template <int LIE>
+  __device__ __forceinline__ void store(void* base, int64_t at, int gap, Part n) const {
+    float* p = static_cast<float*>(base) + at;
+    store_quad<LIE>(p, n.lo, a);
+    store_quad<LIE>(p + gap, n.hi, b);
   }
 };
 
-// A lane's n channels (0 to 8) of a row.
-template <bool BF16>
-__device__ __forceinline__ Piece<BF16> load(const void* base, int64_t at, int n) {
-  Piece<BF16> p;
-  const char* q = static_cast<const char*>(base) + at * (BF16 ? 2 : 4);
-  if (n == 8)
-    p.load(q);
-  else
-    p.load_part(q, n);
-  return p;
-}
-template <bool BF16>
-__device__ __forceinline__ void store(void* base, int64_t at, int n, const Piece<BF16>& p) {
-  char* q = static_cast<char*>(base) + at * (BF16 ? 2 : 4);
-  if (n == 8)
-    p.store(q);
-  else
-    p.store_part(q, n);
-}
-
-__device__ __forceinline__ void load_vector(const float* base, int64_t at, int n, float fill, float (&v)[8]) {
+// A lane's part of a vector, float32 and read again by other rows.
+template <int LIE>
+__device__ __forceinline__ void load_vector(const float* base, int64_t at, int gap, Part n, int64_t size, float fill,
+                                            float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = fill;
   if (!base) return;
-  const Piece<false> p = load<false>(base, at, n);
+  Piece<false> p;
+  p.load<LIE == kLines ? kWhole : LIE>(base, at, gap, n, size);
   p.get(v);
 }
 
 // The sum over a team's lanes, in every one of them.
-template <int LANES>
+template <int LANES>  // at least 8
 __device__ __forceinline__ float lanes_sum(float x) {
   auto add = [](float a, uint32_t b) { return a + __uint_as_float(b); };
   x = add(x, dpp<kSwap1>(__float_as_uint(x)));
   x = add(x, dpp<kSwap2>(__float_as_uint(x)));
-  if (LANES >= 8) x = add(x, dpp<kMirror8>(__float_as_uint(x)));
+  x = add(x, dpp<kMirror8>(__float_as_uint(x)));
   if (LANES >= 16) x = add(x, dpp<kMirror16>(__float_as_uint(x)));
   if (LANES >= 32) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -128,8 +178,7 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // The sum over a wave's teams, of the lanes at the same place of each.
 template <int LANES>
 __device__ __forceinline__ float teams_sum(float x) {
-  constexpr int kTurn4 = 0x124, kTurn8 = 0x128;  // row_ror: lanes 4, 8 apart in a row of 16
-  if (LANES <= 4) x += __uint_as_float(dpp<kTurn4>(__float_as_uint(x)));
+  constexpr int kTurn8 = 0x128;  // row_ror: lanes 8 apart in a row of 16
   if (LANES <= 8) x += __uint_as_float(dpp<kTurn8>(__float_as_uint(x)));
   if (LANES <= 16) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -158,56 +207,83 @@ __device__ __forceinline__ float row_sum(float x, float (*sums)[kMaxWaves], int&
   return x;
 }
 
-// A lane's place in its team, and its channels: from `first` on, `step` apart.
-template <int LANES, bool BLOCK>
+// A lane's place in its team, and its channels: from `first` on, the second 4 of a piece
+// `gap` behind, the pieces `step` apart.
+template <bool BF16, int LANES, bool BLOCK>
 struct Lane {
-  int team, teams, first, step;
+  int team, teams, first, gap, step;
   __device__ __forceinline__ Lane() {
+    const int lanes = BLOCK ? blockDim.x : LANES, lane = BLOCK ? threadIdx.x : threadIdx.x & (LANES - 1);
     team = BLOCK ? 0 : threadIdx.x / LANES;
     teams = BLOCK ? 1 : kWaves * 64 / LANES;
-    first = kSpan * (BLOCK ? threadIdx.x : threadIdx.x & (LANES - 1));
-    step = kSpan * (BLOCK ? blockDim.x : LANES);
+    first = (BF16 ? 8 : 4) * lane;
+    gap = BF16 ? 4 : 4 * lanes;
+    step = 8 * lanes;
   }
-  __device__ __forceinline__ int channels(int i, int width) const {
+  __device__ __forceinline__ Part part(int i, int width) const {
+    auto four = [](int left) { return left < 0 ? 0 : left > 4 ? 4 : left; };
     const int left = width - first - i * step;
-    return left < 0 ? 0 : left > 8 ? 8 : left;
+    return {four(left), four(left - gap)};
   }
 };
 
-template <bool BF16, int LANES, int PIECES, bool BLOCK>
+// The largest |bits| of 4 values, and over 4 and 8 neighbouring lanes.
+__device__ __forceinline__ uint32_t top4(float a, float b, float c, float d) {
+  auto bits = [](float x) { return __float_as_uint(x) & 0x7FFFFFFFu; };
+  return umax(umax(bits(a), bits(b)), umax(bits(c), bits(d)));
+}
+__device__ __forceinline__ uint32_t over_quad(uint32_t t) {
+  t = umax(t, dpp<kSwap1>(t));
+  return umax(t, dpp<kSwap2>(t));
+}
+__device__ __forceinline__ uint32_t over_eight(uint32_t t) {
+  t = over_quad(t);
+  return umax(t, dpp<kMirror8>(t));
+}
+
+// A team takes one row, so that what is in flight is a narrow band of each tensor's rows, and
+// finds the vectors in the caches.  Training tile (2^18 rows of 1024, bf16): 6.3 TB/s; 6.0
+// with 256 blocks that keep the vectors in registers and load a row ahead, 5.4 with 1024.
+// Ragged rows, whose vectors take many instructions to load: where there are more blocks than
+// fit the card a team takes several, loading a row ahead (rows of 33: 4.1 against 3.4 TB/s).
+template <bool BF16, int LANES, int PIECES, bool BLOCK, int LIE>
 __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) fwd_kernel(const NormArgs a) {
   __shared__ float sums[2][kMaxWaves];
   int turn = 0;
-  const Lane<LANES, BLOCK> at;
+  const Lane<BF16, LANES, BLOCK> at;
   const int width = a.width;
-  int n[PIECES];
+  Part n[PIECES];
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) n[i] = at.channels(i, width);
-  const float inv = 1.f / width;
-  const int64_t first = block_index() * at.teams * a.steps + at.team;
-  int64_t held = -1;
+  for (int i = 0; i < PIECES; ++i) n[i] = at.part(i, width);
+  constexpr bool kSeveral = LIE == kRagged;
+  const int64_t size = a.rows * width, stride = a.blocks * at.teams;
+  Piece<BF16> s[PIECES], x[PIECES], next_s[PIECES], next_x[PIECES];
+  auto fetch = [&](int64_t t) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) next_s[i].template load<LIE>(a.res, t * width + at.first + i * at.step, at.gap, n[i], size);
+    if (!a.x) return;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) next_x[i].template load<LIE>(a.x, t * width + at.first + i * at.step, at.gap, n[i], size);
+  };
+  int64_t t = block_index() * at.teams + at.team, held = -1;
   float gate[PIECES][8], scale[PIECES][8], shift[PIECES][8];
-  for (int k = 0; k < a.steps; ++k) {
-    const int64_t t = first + (int64_t)k * at.teams;
-    if (t >= a.rows) break;  // a whole team; with BLOCK the whole block
-    const int64_t row = t * width + at.first;
-    const int64_t b = div_by((uint32_t)t, a.by_group);
+  if (t < a.rows) fetch(t);
+  for (; t < a.rows; t += stride) {
+    const int64_t row = t * width + at.first, b = div_by((uint32_t)t, a.by_group);
     if (b != held) {
       held = b;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const int64_t c = b * width + at.first + i * at.step;
-        load_vector(a.gate, c, n[i], 1.f, gate[i]);
-        load_vector(a.scale, c, n[i], 1.f, scale[i]);
-        load_vector(a.shift, c, n[i], 0.f, shift[i]);
+        load_vector<LIE>(a.gate, c, at.gap, n[i], a.groups * width, 1.f, gate[i]);
+        load_vector<LIE>(a.scale, c, at.gap, n[i], a.groups * width, 1.f, scale[i]);
+        load_vector<LIE>(a.shift, c, at.gap, n[i], a.groups * width, 0.f, shift[i]);
       }
     }
-    Piece<BF16> s[PIECES], x[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) s[i] = load<BF16>(a.res, row + i * at.step, n[i]);
+    for (int i = 0; i < PIECES; ++i) s[i] = next_s[i], x[i] = next_x[i];
+    if (kSeveral && t + stride < a.rows) fetch(t + stride);
     if (a.x) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) x[i] = load<BF16>(a.x, row + i * at.step, n[i]);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         float u[8], v[8];
@@ -216,18 +292,19 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) fwd_kern
 #pragma unroll
         for (int j = 0; j < 8; ++j) u[j] = fmaf(gate[i][j], v[j], u[j]);
         s[i].set(u);
-        store<BF16>(a.sum, row + i * at.step, n[i], s[i]);
+        s[i].template store<LIE>(a.sum, row + i * at.step, at.gap, n[i]);
       }
     }
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float u[8];
+      s[i].template keep<LIE>(n[i]);
       s[i].get(u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = fmaf(u[j], u[j], m);
     }
-    const float r = rsqrtf(row_sum<LANES, BLOCK>(m, sums, turn) * inv + a.eps);
+    const float r = rsqrtf(row_sum<LANES, BLOCK>(m, sums, turn) * a.inverse + a.eps);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float u[8];
@@ -235,108 +312,133 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) fwd_kern
 #pragma unroll
       for (int j = 0; j < 8; ++j) u[j] = fmaf(u[j] * r, scale[i][j], shift[i][j]);
       s[i].set(u);
-      if (a.y) store<BF16>(a.y, row + i * at.step, n[i], s[i]);
-      if (a.codes && n[i]) {  // whole groups: the width is a multiple of 32
+      if (a.y) s[i].template store<LIE>(a.y, row + i * at.step, at.gap, n[i]);
+      if (LIE != kRagged && a.codes && n[i].lo) {  // whole groups: the width is a multiple of 32
         s[i].get(u);
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = umax(top, __float_as_uint(u[j]) & 0x7FFFFFFFu);
-        top = umax(top, dpp<kSwap1>(top));
-        top = umax(top, dpp<kSwap2>(top));
-        const uint32_t e = exponent_of(top);
         const int64_t c = row + i * at.step;
-        *reinterpret_cast<uint2*>(a.codes + c) = encode8(u, e);
-        if ((threadIdx.x & 3) == 0) a.scales[c >> 5] = (uint8_t)e;
+        const uint32_t lo = top4(u[0], u[1], u[2], u[3]), hi = top4(u[4], u[5], u[6], u[7]);
+        if (BF16) {  // 4 lanes a group
+          const uint32_t e = exponent_of(over_quad(umax(lo, hi)));
+          *reinterpret_cast<uint2*>(a.codes + c) = encode8(u, e);
+          if ((threadIdx.x & 3) == 0) a.scales[c >> 5] = (uint8_t)e;
+        } else {  // 8 lanes, of each half
+          const uint32_t e = exponent_of(over_eight(lo)), f = exponent_of(over_eight(hi));
+          *reinterpret_cast<uint32_t*>(a.codes + c) = encode8(u, e).x;
+          if ((threadIdx.x & 7) == 0) a.scales[c >> 5] = (uint8_t)e;
+          if (n[i].hi) {
+            *reinterpret_cast<uint32_t*>(a.codes + c + at.gap) = encode8(u, f).y;
+            if ((threadIdx.x & 7) == 0) a.scales[(c + at.gap) >> 5] = (uint8_t)f;
+          }
+        }
       }
     }
+    if (!kSeveral) return;
   }
 }
 
-// A block takes rows of one group, [chunk * span, ...) of them, its teams in turn; it writes
-// its sums for the vectors' gradients as a row of `partial`, or where it is the group's only
-// block as the gradients.
-template <bool BF16, int LANES, int PIECES, bool BLOCK>
+// What the backward reads of a row.
+template <bool BF16, int PIECES, bool ALL>
+struct Row {
+  Piece<BF16> s[PIECES], up[PIECES], ds[PIECES], x[ALL ? PIECES : 1];
+  template <int LIE>
+  __device__ __forceinline__ void load(const NormArgs& a, int64_t row, int step, int gap, const Part (&n)[PIECES], int64_t size) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) s[i].template load<LIE>(a.total, row + i * step, gap, n[i], size);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) up[i].template load<LIE>(a.dy, row + i * step, gap, n[i], size);
+    if (ALL && a.x) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) x[i].template load<LIE>(a.x, row + i * step, gap, n[i], size);
+    }
+    if (a.dsum) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) ds[i].template load<LIE>(a.dsum, row + i * step, gap, n[i], size);
+    }
+  }
+};
+
+// The blocks of a group take its rows in turn, so that together they read a narrow band of
+// them, each with the next row's loads in flight behind the present one's sums.  A block
+// writes its sums for the vectors' gradients as a row of `partial`, or where it is the
+// group's only block as the gradients.  ALL: with a gate or the shift's gradient, else with
+// the scale's gradient at most, which takes fewer registers.
+template <bool BF16, int LANES, int PIECES, bool BLOCK, int LIE, bool ALL>
 __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) bwd_kernel(const NormArgs a) {
   __shared__ float sums[2][kMaxWaves];
   int turn = 0;
-  const Lane<LANES, BLOCK> at;
+  const Lane<BF16, LANES, BLOCK> at;
   const int width = a.width;
-  int n[PIECES];
+  Part n[PIECES];
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) n[i] = at.channels(i, width);
-  const float inv = 1.f / width;
-  const int64_t block = block_index();
+  for (int i = 0; i < PIECES; ++i) n[i] = at.part(i, width);
+  const int64_t block = block_index(), size = a.rows * width;
   if (block >= a.groups * a.chunks) return;
   const int64_t b = block / a.chunks, chunk = block - b * a.chunks;
-  const int64_t lo = chunk * a.span, hi = lo + a.span < a.group_rows ? lo + a.span : a.group_rows;
-  float gate[PIECES][8], scale[PIECES][8], dgate[PIECES][8] = {}, dscale[PIECES][8] = {}, dshift[PIECES][8] = {};
+  constexpr int kAll = ALL ? PIECES : 1;
+  float gate[kAll][8], scale[PIECES][8], dgate[kAll][8] = {}, dscale[PIECES][8] = {}, dshift[kAll][8] = {};
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     const int64_t c = b * width + at.first + i * at.step;
-    load_vector(a.gate, c, n[i], 1.f, gate[i]);
-    load_vector(a.scale, c, n[i], 1.f, scale[i]);
+    if (ALL) load_vector<LIE>(a.gate, c, at.gap, n[i], a.groups * width, 1.f, gate[i]);
+    load_vector<LIE>(a.scale, c, at.gap, n[i], a.groups * width, 1.f, scale[i]);
   }
-  for (int64_t k = lo + at.team; k < hi; k += at.teams) {
-    const int64_t row = (b * a.group_rows + k) * width + at.first;
-    Piece<BF16> s[PIECES], up[PIECES], ds[PIECES], x[PIECES];
+  const int64_t last = (b + 1) * a.group_rows, stride = a.chunks * at.teams;
+  int64_t t = b * a.group_rows + chunk * at.teams + at.team;
+  Row<BF16, PIECES, ALL> next;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) s[i] = load<BF16>(a.total, row + i * at.step, n[i]);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) up[i] = load<BF16>(a.dy, row + i * at.step, n[i]);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      ds[i].clear();
-      if (a.dsum) ds[i] = load<BF16>(a.dsum, row + i * at.step, n[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      x[i].clear();
-      if (a.x) x[i] = load<BF16>(a.x, row + i * at.step, n[i]);
-    }
+  for (int i = 0; i < PIECES; ++i) next.ds[i].clear();
+  if (t < last) next.template load<LIE>(a, t * width + at.first, at.step, at.gap, n, size);
+  for (; t < last; t += stride) {
+    // the loads before this row's stores: both count alike, and a wait for loads behind stores waits for these too
+    Row<BF16, PIECES, ALL> in = next;
+    if (t + stride < last) next.template load<LIE>(a, (t + stride) * width + at.first, at.step, at.gap, n, size);
+    const int64_t row = t * width + at.first;
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float v[8];
-      s[i].get(v);
+      in.s[i].template keep<LIE>(n[i]);
+      in.up[i].template keep<LIE>(n[i]);
+      in.s[i].get(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = fmaf(v[j], v[j], m);
     }
-    const float r = rsqrtf(row_sum<LANES, BLOCK>(m, sums, turn) * inv + a.eps);
+    const float r = rsqrtf(row_sum<LANES, BLOCK>(m, sums, turn) * a.inverse + a.eps);
     // with y = r s, u = r scale dy: dres = u - y mean(u y) + dsum, r never squared: it may reach 2^74
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float v[8], u[8];
-      s[i].get(v);
-      up[i].get(u);
+      in.s[i].get(v);
+      in.up[i].get(u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) dot = fmaf(u[j] * scale[i][j] * r, v[j] * r, dot);
     }
-    dot = row_sum<LANES, BLOCK>(dot, sums, turn) * inv;
+    dot = row_sum<LANES, BLOCK>(dot, sums, turn) * a.inverse;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float v[8], u[8], h[8];
-      s[i].get(v);
-      up[i].get(u);
-      ds[i].get(h);
+      in.s[i].get(v);
+      in.up[i].get(u);
+      in.ds[i].get(h);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         v[j] *= r;
         dscale[i][j] = fmaf(u[j], v[j], dscale[i][j]);
-        dshift[i][j] += u[j];
+        if (ALL) dshift[i][j] += u[j];
         h[j] += fmaf(-v[j], dot, u[j] * scale[i][j] * r);
       }
-      s[i].set(h);
-      store<BF16>(a.dres, row + i * at.step, n[i], s[i]);
-      if (a.dx) {
-        x[i].get(v);
+      in.s[i].set(h);
+      in.s[i].template store<LIE>(a.dres, row + i * at.step, at.gap, n[i]);
+      if (ALL && a.x) {
+        in.x[i].get(v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           dgate[i][j] = fmaf(h[j], v[j], dgate[i][j]);
           h[j] *= gate[i][j];
         }
-        s[i].set(h);
-        store<BF16>(a.dx, row + i * at.step, n[i], s[i]);
+        in.s[i].set(h);
+        in.s[i].template store<LIE>(a.dx, row + i * at.step, at.gap, n[i]);
       }
     }
   }
@@ -346,18 +448,19 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) bwd_kern
 #pragma unroll
   for (int which = 0; which < 3; ++which) {
     float* out = which == 0 ? a.dgate : which == 1 ? a.dscale : a.dshift;
-    if (!out) continue;
+    if (!out || (which != 1 && !ALL)) continue;
     out = a.chunks == 1 ? out + b * width : a.partial + (row++ * a.groups * a.chunks + block) * width;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      float(&d)[8] = which == 0 ? dgate[i] : which == 1 ? dscale[i] : dshift[i];
+      float(&d)[8] = which == 0 ? dgate[ALL ? i : 0] : which == 1 ? dscale[i] : dshift[ALL ? i : 0];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        const int c = at.first + i * at.step + (j < 4 ? j : at.gap + j - 4);
         if (BLOCK) {
-          if (j < n[i]) out[at.first + i * at.step + j] = d[j];
+          if (c < width) out[c] = d[j];
         } else {
           const float x = teams_sum<LANES>(d[j]);
-          if ((threadIdx.x & 63) < LANES) wide[threadIdx.x >> 6][at.first + i * at.step + j] = x;
+          if ((threadIdx.x & 63) < LANES) wide[threadIdx.x >> 6][c] = x;
         }
       }
     }
@@ -403,61 +506,101 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const NormArgs a) {
   out[group * a.width + col] = y;
 }
 
-// Waves that keep the card full, and blocks of the backward, which write a row of partial sums each.
-constexpr int64_t kFill = 8192, kBwdBlocks = 1024;
-
-static int lanes_of(int width) {
-  int l = 4;
-  while (l < 64 && l * kSpan < width) l *= 2;
-  return l;
+// A launch: lanes and pieces of a row, or where it is wider than a wave takes the waves of
+// its block.
+struct Shape {
+  int lanes, pieces, threads, teams;
+};
+static Shape shape_of(int width, bool back) {
+  constexpr int kWave = 64 * 8;  // channels of a wave's piece
+  if (width > 2 * kWave) return {64, 2, 64 * ((width + 2 * kWave - 1) / (2 * kWave)), 1};
+  // Two pieces a lane in the backward where rows are long enough for 8 lanes: half as many exchanges an element, and a
+  // wave has twice as much in flight.  The forward has more waves in flight instead (rows of 512: 6.5 and 6.2 TB/s).
+  const int most = width > 64 && back ? 2 : 1;
+  int lanes = 8;
+  while (lanes < 64 && lanes * 8 * most < width) lanes *= 2;
+  return {lanes, lanes * 8 < width ? 2 : 1, kWaves * 64, kWaves * 64 / lanes};
 }
-static bool by_block(int width) { return width > 2 * 64 * kSpan; }
-static int threads_of(int width) { return by_block(width) ? 64 * ((width + 2 * 64 * kSpan - 1) / (2 * 64 * kSpan)) : kWaves * 64; }
-static int teams_of(int width) { return by_block(width) ? 1 : kWaves * 64 / lanes_of(width); }
+
+// Blocks of the forward: a row for each team, but short ragged rows.
+static int64_t fwd_blocks(const NormArgs& a) {
+  const int teams = shape_of(a.width, false).teams;
+  const int64_t all = (a.rows + teams - 1) / teams;
+  return a.width % 8 && a.width <= 512 && all > 1024 ? 1024 : all;
+}
+
+// Blocks of the backward, which write a row of partial sums each: few waves with much in flight each read faster than
+// many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.9, 5.6), two
+// where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's two more streams and
+// three sums (rows of 4096 5.9, 5.5, 5.3); ragged rows two (rows of 201: 4.3, 5.0, 4.8) if they are many.
+constexpr int kCus = 256;
+static int64_t bwd_blocks(const NormArgs& a) {
+  const Shape at = shape_of(a.width, true);
+  if (at.teams > 1) return a.width % 8 && a.rows >= (int64_t)2 * kCus * 8 * at.teams ? 2 * kCus : kCus;
+  const int waves = at.threads / 64, want = a.gate || a.dshift ? 4 : 8;
+  return waves >= want ? kCus : kCus * (want / waves);
+}
 
 static void plan_bwd(NormArgs& a) {
-  const int teams = teams_of(a.width);
+  const int teams = shape_of(a.width, true).teams;
   const int64_t most = (a.group_rows + teams - 1) / teams;
   // partial sums of 16 MiB, or a block's for 12 rows, a tenth of what these move in bf16
   const int64_t room = (16 << 20) / (3 * 4 * a.width), tenth = a.rows / 12;
-  int64_t want = room > tenth ? room : tenth;
-  want = (want < kBwdBlocks ? want : kBwdBlocks) / a.groups;
-  a.chunks = want < 1 ? 1 : want < most ? want : most;
-  a.span = (a.group_rows + a.chunks - 1) / a.chunks;
-  a.chunks = (a.group_rows + a.span - 1) / a.span;
+  const int64_t room_for = room > tenth ? room : tenth, fill = bwd_blocks(a);
+  // as many for each group as fit, or one more where a fifth of the card would be idle
+  int64_t want = (room_for < fill ? room_for : fill) / a.groups;
+  if (want == 0 || 5 * want * a.groups < 4 * (room_for < fill ? room_for : fill)) ++want;
+  a.chunks = want < most ? want : most;
 }
 
-template <bool BF16, int LANES, int PIECES, bool BLOCK>
-static void start(const NormArgs& a, bool back, dim3 grid, hipStream_t s) {
-  const dim3 block(threads_of(a.width));
-  if (back)
-    hipLaunchKernelGGL((bwd_kernel<BF16, LANES, PIECES, BLOCK>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((fwd_kernel<BF16, LANES, PIECES, BLOCK>), grid, block, 0, s, a);
+// Rows past the caches' replacement: of whole lines, where the tensor is too large to be found there again.
+static bool streams(const NormArgs& a) { return a.width % 64 == 0 && a.rows * a.width >= (1 << 26); }
+
+template <bool BF16, int LANES, int PIECES, bool BLOCK, int LIE>
+static void start(const NormArgs& a, bool back, const Shape& at, hipStream_t s) {
+  const dim3 grid = grid_of(back ? a.groups * a.chunks : a.blocks), block(at.threads);
+  if (!back) {
+    if constexpr (PIECES == 1 || LANES == 64)
+      hipLaunchKernelGGL((fwd_kernel<BF16, LANES, PIECES, BLOCK, LIE>), grid, block, 0, s, a);
+  } else if (a.gate || a.dshift) {
+    hipLaunchKernelGGL((bwd_kernel<BF16, LANES, PIECES, BLOCK, LIE, true>), grid, block, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((bwd_kernel<BF16, LANES, PIECES, BLOCK, LIE, false>), grid, block, 0, s, a);
+  }
+}
+
+template <bool BF16, int LIE>
+static void run(const NormArgs& a, bool back, hipStream_t s) {
+  const Shape at = shape_of(a.width, back);
+  if (at.teams == 1) return start<BF16, 64, 2, true, LIE>(a, back, at, s);
+  if (at.pieces == 1) {
+    switch (at.lanes) {
+      case 8: return start<BF16, 8, 1, false, LIE>(a, back, at, s);
+      case 16: return start<BF16, 16, 1, false, LIE>(a, back, at, s);
+      case 32: return start<BF16, 32, 1, false, LIE>(a, back, at, s);
+      default: return start<BF16, 64, 1, false, LIE>(a, back, at, s);
+    }
+  }
+  switch (at.lanes) {
+    case 8: return start<BF16, 8, 2, false, LIE>(a, back, at, s);
+    case 16: return start<BF16, 16, 2, false, LIE>(a, back, at, s);
+    case 32: return start<BF16, 32, 2, false, LIE>(a, back, at, s);
+    default: return start<BF16, 64, 2, false, LIE>(a, back, at, s);
+  }
 }
 
 template <bool BF16>
-static void run(const NormArgs& a, bool back, dim3 grid, hipStream_t s) {
-  if (by_block(a.width)) return start<BF16, 64, 2, true>(a, back, grid, s);
-  switch (lanes_of(a.width)) {
-    case 4: return start<BF16, 4, 1, false>(a, back, grid, s);
-    case 8: return start<BF16, 8, 1, false>(a, back, grid, s);
-    case 16: return start<BF16, 16, 1, false>(a, back, grid, s);
-    case 32: return start<BF16, 32, 1, false>(a, back, grid, s);
-    default:
-      if (a.width <= 64 * kSpan) return start<BF16, 64, 1, false>(a, back, grid, s);
-      return start<BF16, 64, 2, false>(a, back, grid, s);
-  }
+static void run(const NormArgs& a, bool back, hipStream_t s) {
+  if (a.width % 8) return run<BF16, kRagged>(a, back, s);
+  streams(a) ? run<BF16, kLines>(a, back, s) : run<BF16, kWhole>(a, back, s);
 }
 
 }  // namespace row_norm
 
 void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s) {
-  const int64_t teams = row_norm::teams_of(a.width), waves = a.rows * row_norm::threads_of(a.width) / 64 / teams;
-  a.steps = waves / row_norm::kFill < 1 ? 1 : waves / row_norm::kFill > 8 ? 8 : (int)(waves / row_norm::kFill);
   a.by_group = fast_div(a.group_rows);
-  const dim3 grid = ckpt8::grid_of((a.rows + teams * a.steps - 1) / (teams * a.steps));
-  dt == STRATA_BF16 ? row_norm::run<true>(a, false, grid, s) : row_norm::run<false>(a, false, grid, s);
+  a.blocks = row_norm::fwd_blocks(a);
+  dt == STRATA_BF16 ? row_norm::run<true>(a, false, s) : row_norm::run<false>(a, false, s);
 }
 
 size_t residual_norm_partial_bytes(NormArgs a) {
@@ -467,8 +610,7 @@ size_t residual_norm_partial_bytes(NormArgs a) {
 
 void launch_residual_norm_bwd(NormArgs a, strata_dtype dt, hipStream_t s) {
   row_norm::plan_bwd(a);
-  const dim3 grid = ckpt8::grid_of(a.groups * a.chunks);
-  dt == STRATA_BF16 ? row_norm::run<true>(a, true, grid, s) : row_norm::run<false>(a, true, grid, s);
+  dt == STRATA_BF16 ? row_norm::run<true>(a, true, s) : row_norm::run<false>(a, true, s);
   const unsigned vectors = !!a.dgate + !!a.dscale + !!a.dshift;
   if (a.chunks == 1 || !vectors) return;
   hipLaunchKernelGGL(row_norm::sum_kernel, dim3((a.width + 31) / 32, (unsigned)a.groups, vectors),
