@@ -79,7 +79,7 @@ def encode(x, random, second):
     if second:
         code = np.where(a > 0, np.maximum(code, 1), code)
     else:
-        code = code + np.where(v < 0, 128, 0)
+        code = code + np.where(np.signbit(v), 128, 0)
     code = np.where(fine[:, None], code, 0)
     return code.astype(np.uint8).reshape(-1), np.where(fine, e, 255).astype(np.uint8)
 

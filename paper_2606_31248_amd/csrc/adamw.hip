@@ -14,24 +14,44 @@ namespace adamw {
 
 using namespace ckpt8;
 
-constexpr int kThreads = 256, kSpan = 4 * kThreads, kParts = kParamChunk / kSpan;
+constexpr int kThreads = 256, kSpan = 4 * kThreads;
+
+// A pointer out of the table, which lies in the device's memory like all that kernels are given.
+template <typename T>
+using Global = T __attribute__((address_space(1)))*;
+template <typename T, typename P>
+__device__ __forceinline__ Global<T> global(P* p) {
+  return (Global<T>)reinterpret_cast<uintptr_t>(p);
+}
+
+// 16, 8 or 4 bytes that are touched once a step, past the caches' replacement.
+template <typename T>
+__device__ __forceinline__ T load(Global<const T> p) {
+  return __builtin_nontemporal_load(p);
+}
+template <typename T>
+__device__ __forceinline__ void store(Global<T> p, T v) {
+  __builtin_nontemporal_store(v, p);
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // A lane's 4 gradients, n of them there.
 __device__ __forceinline__ void load_grads(const ParamRecord& t, int64_t at, int n, float (&g)[4]) {
   if (t.bf16) {
-    const uint16_t* q = static_cast<const uint16_t*>(t.g) + at;
+    const Global<const uint16_t> q = global<const uint16_t>(t.g) + at;
     if (n == 4) {
-      const uint2 w = *reinterpret_cast<const uint2*>(q);
+      const u32x2 w = load<u32x2>((Global<const u32x2>)q);
       g[0] = mfma::lo_bf16(w.x), g[1] = mfma::hi_bf16(w.x), g[2] = mfma::lo_bf16(w.y), g[3] = mfma::hi_bf16(w.y);
       return;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) g[j] = j < n ? bf16_to_f32(q[j]) : 0.f;
   } else {
-    const float* q = static_cast<const float*>(t.g) + at;
+    const Global<const float> q = global<const float>(t.g) + at;
     if (n == 4) {
-      const float4 w = *reinterpret_cast<const float4*>(q);
-      g[0] = w.x, g[1] = w.y, g[2] = w.z, g[3] = w.w;
+      const u32x4 w = load<u32x4>((Global<const u32x4>)q);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[j] = __uint_as_float(w[j]);
       return;
     }
 #pragma unroll
@@ -39,19 +59,23 @@ __device__ __forceinline__ void load_grads(const ParamRecord& t, int64_t at, int
   }
 }
 
-__device__ __forceinline__ void load_floats(const float* q, int n, float (&v)[4]) {
+__device__ __forceinline__ void load_floats(const float* base, int64_t at, int n, float (&v)[4]) {
+  const Global<const float> q = global<const float>(base) + at;
   if (n == 4) {
-    const float4 w = *reinterpret_cast<const float4*>(q);
-    v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+    const u32x4 w = load<u32x4>((Global<const u32x4>)q);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
     return;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = j < n ? q[j] : 0.f;
 }
 
-__device__ __forceinline__ void store_floats(float* q, int n, const float (&v)[4]) {
+__device__ __forceinline__ void store_floats(float* base, int64_t at, int n, const float (&v)[4]) {
+  const Global<float> q = global<float>(base) + at;
   if (n == 4) {
-    *reinterpret_cast<float4*>(q) = make_float4(v[0], v[1], v[2], v[3]);
+    store<u32x4>((Global<u32x4>)q, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                                                 __float_as_uint(v[3])});
     return;
   }
 #pragma unroll
@@ -59,9 +83,10 @@ __device__ __forceinline__ void store_floats(float* q, int n, const float (&v)[4
     if (j < n) q[j] = v[j];
 }
 
-__device__ __forceinline__ void store_copy(uint16_t* q, int n, const float (&v)[4]) {
+__device__ __forceinline__ void store_copy(uint16_t* base, int64_t at, int n, const float (&v)[4]) {
+  const Global<uint16_t> q = global<uint16_t>(base) + at;
   if (n == 4) {
-    *reinterpret_cast<uint2*>(q) = make_uint2(mfma::pack2(v[0], v[1]), mfma::pack2(v[2], v[3]));
+    store<u32x2>((Global<u32x2>)q, u32x2{mfma::pack2(v[0], v[1]), mfma::pack2(v[2], v[3])});
     return;
   }
 #pragma unroll
@@ -91,49 +116,50 @@ template <bool SECOND>
 __device__ __forceinline__ void store4(void* codes, uint8_t* scales, int64_t place, const float (&v)[4],
                                        const uint32_t (&random)[4]) {
   const uint32_t e = state8::exponent_of<SECOND>(group_top(v));
+  const float per_unit = state8::per_unit_of<SECOND>(e);
   uint32_t w = 0;
-  if (e != 255u) {
-    const float per_unit = state8::per_unit_of<SECOND>(e);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w |= state8::encode<SECOND>(v[j], per_unit, random[j]) << (8 * j);
-  }
-  *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(codes) + place) = w;
-  if ((threadIdx.x & 7) == 0) scales[place >> 5] = (uint8_t)e;
+  for (int j = 0; j < 4; ++j) w |= state8::encode<SECOND>(v[j], per_unit, random[j]) << (8 * j);
+  store<uint32_t>(global<uint32_t>(static_cast<uint8_t*>(codes) + place), e == 255u ? 0u : w);
+  if ((threadIdx.x & 7) == 0) global<uint8_t>(scales)[place >> 5] = (uint8_t)e;
 }
 
-template <bool EIGHT>
-__global__ void __launch_bounds__(kThreads) step_kernel(const AdamArgs a) {
-  const int64_t chunk = block_index();
-  if (chunk >= a.chunks) return;
-  const float factor = a.factor ? *a.factor : 1.f;
-  if (factor != factor) return;  // gradients that are not finite: nothing changes
-  const ParamRecord t = a.tensors[a.owner[chunk]];
-  const int64_t first = (chunk - t.chunk) * kParamChunk + 4 * threadIdx.x;
+// (m rate) / (sqrt(v) root + eps), to 4 roundings.  The square root's instruction takes
+// normal numbers: a v below 2^-96 is scaled by 2^64, its root back.
+__device__ __forceinline__ float step_of(float m, float v, const AdamArgs& a) {
+  const bool tiny = v < 0x1p-96f;
+  const float s = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v);
+  return a.rate * m * __builtin_amdgcn_rcpf(fmaf(s, tiny ? a.root * 0x1p-32f : a.root, a.eps));
+}
+
+// A lane's part of a chunk.  WHOLE: all its elements are there.
+template <bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void step_chunk(const AdamArgs& a, const ParamRecord& t, int64_t first, float factor) {
+  constexpr int kParts = kParamChunk / kSpan;
   float p[kParts][4], g[kParts][4], m[kParts][4], v[kParts][4];
   uint32_t mc[kParts], vc[kParts], me[kParts], ve[kParts];
   int n[kParts];
+  bool here[kParts];  // a lane of a group with elements; places behind a tensor's last hold zeros, and keep them
 #pragma unroll
   for (int i = 0; i < kParts; ++i) {
     const int64_t at = first + i * kSpan, left = t.n - at, place = t.place + at;
-    n[i] = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    if (EIGHT ? t.n <= (at & -32) : n[i] == 0) {  // lanes of a group stay together
-      n[i] = -1;
-      continue;
-    }
+    n[i] = WHOLE || left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    here[i] = WHOLE || t.n > (EIGHT ? at & -32 : at);
+    if (!here[i]) continue;
     load_grads(t, at, n[i], g[i]);
-    load_floats(t.p + at, n[i], p[i]);
+    load_floats(t.p, at, n[i], p[i]);
     if (EIGHT) {
-      mc[i] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.m) + place);
-      vc[i] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + place);
+      mc[i] = load<uint32_t>(global<const uint32_t>(static_cast<const uint8_t*>(a.m) + place));
+      vc[i] = load<uint32_t>(global<const uint32_t>(static_cast<const uint8_t*>(a.v) + place));
       me[i] = a.m_scales[place >> 5], ve[i] = a.v_scales[place >> 5];
     } else {
-      load_floats(static_cast<const float*>(a.m) + place, n[i], m[i]);
-      load_floats(static_cast<const float*>(a.v) + place, n[i], v[i]);
+      load_floats(static_cast<const float*>(a.m), place, 4, m[i]);
+      load_floats(static_cast<const float*>(a.v), place, 4, v[i]);
     }
   }
 #pragma unroll
   for (int i = 0; i < kParts; ++i) {
-    if (n[i] < 0) continue;
+    if (!here[i]) continue;
     const int64_t at = first + i * kSpan, place = t.place + at;
     if (EIGHT) decode4<false>(mc[i], me[i], m[i]), decode4<true>(vc[i], ve[i], v[i]);
 #pragma unroll
@@ -143,12 +169,10 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const AdamArgs a) {
       const float x = g[i][j] * factor;
       m[i][j] = a.beta1 * m[i][j] + a.new1 * x;
       v[i][j] = a.beta2 * v[i][j] + a.new2 * x * x;
-      if (EIGHT && j >= n[i]) m[i][j] = v[i][j] = 0.f;
-      const float root = sqrtf(v[i][j]) * a.root + a.eps;
-      p[i][j] = p[i][j] - (a.decay * p[i][j] + a.rate * m[i][j] / root);
+      p[i][j] = p[i][j] - (a.decay * p[i][j] + step_of(m[i][j], v[i][j], a));
     }
-    store_floats(t.p + at, n[i], p[i]);
-    if (t.copy) store_copy(t.copy + at, n[i], p[i]);
+    store_floats(t.p, at, n[i], p[i]);
+    if (t.copy) store_copy(t.copy, at, n[i], p[i]);
     if (EIGHT) {
       uint32_t low[4], high[4];
 #pragma unroll
@@ -159,27 +183,58 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const AdamArgs a) {
       store4<false>(a.m, a.m_scales, place, m[i], low);
       store4<true>(a.v, a.v_scales, place, v[i], high);
     } else {
-      store_floats(static_cast<float*>(a.m) + place, n[i], m[i]);
-      store_floats(static_cast<float*>(a.v) + place, n[i], v[i]);
+      store_floats(static_cast<float*>(a.m), place, 4, m[i]);
+      store_floats(static_cast<float*>(a.v), place, 4, v[i]);
     }
   }
 }
 
-// Values of a state: a lane 8 codes, any n.
+template <bool EIGHT>
+__global__ void __launch_bounds__(kThreads) step_kernel(const AdamArgs a) {
+  const int64_t chunk = block_index();
+  if (chunk >= a.chunks) return;
+  const float factor = a.factor ? *a.factor : 1.f;
+  if (factor != factor) return;  // gradients that are not finite: nothing changes
+  const ParamRecord t = a.tensors[a.owner[chunk]];
+  const int64_t base = (chunk - t.chunk) * kParamChunk;
+  // without the checks 8 bits take 865 us instead of 925 (24 blocks of 1024 channels), 32 bits 1550 instead of 1518
+  if (EIGHT && base + kParamChunk <= t.n)
+    step_chunk<EIGHT, true>(a, t, base + 4 * threadIdx.x, factor);
+  else
+    step_chunk<EIGHT, false>(a, t, base + 4 * threadIdx.x, factor);
+}
+
+// Values of a state.  A block takes two runs of 2048 codes, of which neighbouring lanes load
+// 16 of one each and swap half, so that a lane has 8 of both.
+constexpr int kHalf = 8 * kThreads, kPair = 2 * kHalf;
+
+template <bool SECOND>
+__device__ __forceinline__ void decode8(uint2 c, float unit, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = state8::decode<SECOND>((j < 4 ? c.x : c.y) >> (8 * (j & 3)) & 255u, unit);
+}
+
 template <bool BF16, bool SECOND>
 __global__ void __launch_bounds__(kThreads) unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n, void* x) {
-  const int64_t at = (block_index() * kThreads + threadIdx.x) * 8;
-  if (at >= n) return;
-  const float unit = state8::unit_of<SECOND>(scales[at >> 5]);
-  if (at + 8 <= n) {
-    const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = state8::decode<SECOND>((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, unit);
-    store8_stream<BF16>(static_cast<char*>(x) + at * (BF16 ? 2 : 4), v);
+  constexpr int kBytes = BF16 ? 2 : 4;
+  const int64_t base = block_index() * kPair, at = base + 8 * threadIdx.x;
+  if (base + kPair > n) {
+    for (int i = 0; i < 2; ++i)
+      for (int64_t k = at + i * kHalf, j = k; j < k + 8 && j < n; ++j)
+        store1<BF16>(x, j, state8::decode<SECOND>(codes[j], state8::unit_of<SECOND>(scales[j >> 5])));
     return;
   }
-  for (int j = 0; at + j < n; ++j) store1<BF16>(x, at + j, state8::decode<SECOND>(codes[at + j], unit));
+  const int odd = threadIdx.x & 1;
+  const u32x4 w = load16(codes + at + (odd ? kHalf - 8 : 0));
+  const uint8_t e[2] = {scales[at >> 5], scales[(at + kHalf) >> 5]};
+  uint2 c[2] = {make_uint2(w.x, w.y), make_uint2(w.z, w.w)};
+  swap_pair(odd, c[0], c[1]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float v[8];
+    decode8<SECOND>(c[i], state8::unit_of<SECOND>(e[i]), v);
+    store8_stream<BF16>(static_cast<char*>(x) + (at + i * kHalf) * kBytes, v);
+  }
 }
 
 __device__ __forceinline__ double block_sum(double x) {
@@ -194,25 +249,57 @@ __device__ __forceinline__ double block_sum(double x) {
   return sums[0];
 }
 
+__device__ __forceinline__ void add_square(double& x, float v) { x = fma((double)v, (double)v, x); }
+
 // Squares of float32 values in float64: neither range nor digits are lost, whatever the count.
+// A block takes kRun neighbouring chunks at a time: where they are of one tensor, all of a
+// lane's loads, 16 bytes each, are in flight together.
+constexpr int kRun = 4;
+template <bool BF16>
+__device__ __forceinline__ void square_run(const ParamRecord& t, int64_t base, double& x, double& y) {
+  constexpr int kLoads = kRun * kParamChunk / kSpan / (BF16 ? 2 : 1);
+  const Global<const u32x4> q = global<const u32x4>(static_cast<const char*>(t.g) + base * (BF16 ? 2 : 4)) + threadIdx.x;
+  u32x4 w[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) w[i] = load<u32x4>(q + i * kThreads);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (BF16)
+        add_square(x, mfma::lo_bf16(w[i][j])), add_square(y, mfma::hi_bf16(w[i][j]));
+      else
+        add_square(j & 1 ? y : x, __uint_as_float(w[i][j]));
+    }
+  }
+}
+
 __global__ void __launch_bounds__(kThreads) squares_kernel(const ParamRecord* tensors, const int32_t* owner,
                                                            int64_t chunks, double* partial) {
-  double x = 0.;
-  for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-    const ParamRecord t = tensors[owner[chunk]];
-    const int64_t first = (chunk - t.chunk) * kParamChunk + 4 * threadIdx.x;
-    float g[kParts][4];
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      const int64_t at = first + i * kSpan, left = t.n - at;
-      load_grads(t, at, left >= 4 ? 4 : left > 0 ? (int)left : 0, g[i]);
+  constexpr int kParts = kParamChunk / kSpan, kAll = kRun * kParamChunk;
+  double x = 0., y = 0.;
+  for (int64_t run = (int64_t)blockIdx.x * kRun; run < chunks; run += (int64_t)gridDim.x * kRun) {
+    const int64_t last = run + kRun <= chunks ? run + kRun - 1 : chunks - 1;
+    const ParamRecord t = tensors[owner[run]];
+    const int64_t base = (run - t.chunk) * kParamChunk;
+    if (last == run + kRun - 1 && owner[last] == owner[run] && base + kAll <= t.n) {
+      t.bf16 ? square_run<true>(t, base, x, y) : square_run<false>(t, base, x, y);
+      continue;
     }
+    for (int64_t chunk = run; chunk <= last; ++chunk) {
+      const ParamRecord u = tensors[owner[chunk]];
+      const int64_t first = (chunk - u.chunk) * kParamChunk + 4 * threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i)
+      for (int i = 0; i < kParts; ++i) {
+        const int64_t at = first + i * kSpan, left = u.n - at;
+        float g[4];
+        load_grads(u, at, left >= 4 ? 4 : left > 0 ? (int)left : 0, g);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x = fma((double)g[i][j], (double)g[i][j], x);
+        for (int j = 0; j < 4; ++j) add_square(j & 1 ? y : x, g[j]);
+      }
+    }
   }
-  x = block_sum(x);
+  x = block_sum(x + y);
   if (threadIdx.x == 0) partial[blockIdx.x] = x;
 }
 
@@ -225,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double* partial, i
   norm[1] = !(x <= 0x1.fffffffffffffp1023) ? __uint_as_float(0x7FC00000u) : x <= most ? 1.f : (float)(most / x);
 }
 
-constexpr int kNormBlocks = 2048;
+constexpr int kNormBlocks = 1024;
 
 }  // namespace adamw
 
@@ -243,7 +330,7 @@ void launch_adamw(const AdamArgs& a, hipStream_t s) {
 
 void launch_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n, bool second, void* x, strata_dtype dt,
                          hipStream_t s) {
-  const dim3 grid = ckpt8::grid_of((n + 8 * adamw::kThreads - 1) / (8 * adamw::kThreads)), block(adamw::kThreads);
+  const dim3 grid = ckpt8::grid_of((n + adamw::kPair - 1) / adamw::kPair), block(adamw::kThreads);
   if (dt == STRATA_BF16) {
     if (second)
       hipLaunchKernelGGL((adamw::unpack_kernel<true, true>), grid, block, 0, s, codes, scales, n, x);
@@ -256,7 +343,10 @@ void launch_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n,
   }
 }
 
-int64_t grad_norm_blocks(int64_t chunks) { return chunks < adamw::kNormBlocks ? chunks : adamw::kNormBlocks; }
+int64_t grad_norm_blocks(int64_t chunks) {
+  const int64_t runs = (chunks + adamw::kRun - 1) / adamw::kRun;
+  return runs < adamw::kNormBlocks ? runs : adamw::kNormBlocks;
+}
 
 void launch_grad_norm(const ParamRecord* tensors, const int32_t* owner, int64_t chunks, double most, float* norm,
                       double* partial, hipStream_t s) {

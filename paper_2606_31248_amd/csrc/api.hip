@@ -701,7 +701,7 @@ strata_status strata_residual_norm(const strata_norm_desc* desc, const void* x, 
 size_t strata_residual_norm_bwd_workspace_size(const strata_norm_desc* desc) {
   NormArgs a;
   if (check_norm(desc, &a) != STRATA_OK) return 0;
-  return (residual_norm_partial_bytes(a) + 255) & ~(size_t)255;
+  return (residual_norm_partial_bytes(a, desc->dtype) + 255) & ~(size_t)255;
 }
 
 strata_status strata_residual_norm_bwd(const strata_norm_desc* desc, const void* sum, const void* x, const float* gate,
@@ -720,7 +720,7 @@ strata_status strata_residual_norm_bwd(const strata_norm_desc* desc, const void*
           "x, gate, scale, dsum, dx: not 16-byte aligned");
   REQUIRE(aligned16(dgate) && aligned16(dscale) && aligned16(dshift), "dgate, dscale, dshift: not 16-byte aligned");
   if (dgate || dscale || dshift) {
-    const size_t need = residual_norm_partial_bytes(a);
+    const size_t need = residual_norm_partial_bytes(a, desc->dtype);
     if (need && (!workspace || workspace_bytes < need))
       return set_error(STRATA_ERR_WORKSPACE, "workspace: %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
     REQUIRE(aligned16(workspace), "workspace: not 16-byte aligned");

@@ -105,12 +105,12 @@ struct NormArgs {
   FastDiv by_group;
 };
 void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s);
-size_t residual_norm_partial_bytes(NormArgs a);
+size_t residual_norm_partial_bytes(const NormArgs& a, strata_dtype dt);
 void launch_residual_norm_bwd(NormArgs a, strata_dtype dt, hipStream_t s);
 
 // AdamW over many tensors (adamw.hip).  The table on the device: one record a tensor, then the
 // tensor's index for every chunk of kParamChunk elements of the tensors with a gradient.
-constexpr int kParamChunk = 2048;
+constexpr int kParamChunk = 1024;
 struct ParamRecord {
   float* p;
   const void* g;

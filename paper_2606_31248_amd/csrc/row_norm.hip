@@ -6,6 +6,8 @@
 // registers between its statistics and its results; rows wider than one wave are shared by
 // the waves of a block, which add their sums in LDS.  A team takes several rows, with the
 // channels' gate, scale and shift (backward: and their gradients' sums) in registers.
+#include <algorithm>
+
 #include "ckpt8.h"
 #include "kernels.h"
 
@@ -530,27 +532,31 @@ static int64_t fwd_blocks(const NormArgs& a) {
 }
 
 // Blocks of the backward, which write a row of partial sums each: few waves with much in flight each read faster than
-// many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.9, 5.6), two
-// where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's two more streams and
-// three sums (rows of 4096 5.9, 5.5, 5.3); ragged rows two (rows of 201: 4.3, 5.0, 4.8) if they are many.
+// many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.8, 5.5; with a
+// gate 5.9, 5.0, 5.4), two where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's
+// two more streams and three sums (rows of 4096 5.9, 5.5, 5.3).  If rows are many, ragged ones two (rows of 201: 4.3,
+// 5.0, 4.8) and gated ones of float32 four (5.2, 5.7, 6.0).
 constexpr int kCus = 256;
-static int64_t bwd_blocks(const NormArgs& a) {
+static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
   const Shape at = shape_of(a.width, true);
-  if (at.teams > 1) return a.width % 8 && a.rows >= (int64_t)2 * kCus * 8 * at.teams ? 2 * kCus : kCus;
-  const int waves = at.threads / 64, want = a.gate || a.dshift ? 4 : 8;
-  return waves >= want ? kCus : kCus * (want / waves);
+  if (at.teams == 1) {
+    const int waves = at.threads / 64, want = all ? 4 : 8;
+    return waves >= want ? kCus : kCus * (want / waves);
+  }
+  const int want = a.width % 8 ? 2 : all && !bf16 ? 4 : 1;
+  return a.rows >= (int64_t)kCus * want * 8 * at.teams ? kCus * want : kCus;
 }
 
-static void plan_bwd(NormArgs& a) {
+static int64_t chunks_of(const NormArgs& a, bool bf16, bool all) {
   const int teams = shape_of(a.width, true).teams;
   const int64_t most = (a.group_rows + teams - 1) / teams;
   // partial sums of 16 MiB, or a block's for 12 rows, a tenth of what these move in bf16
-  const int64_t room = (16 << 20) / (3 * 4 * a.width), tenth = a.rows / 12;
-  const int64_t room_for = room > tenth ? room : tenth, fill = bwd_blocks(a);
+  const int64_t room = std::max<int64_t>((16 << 20) / (3 * 4 * a.width), a.rows / 12);
+  const int64_t fill = std::min(room, bwd_blocks(a, bf16, all));
   // as many for each group as fit, or one more where a fifth of the card would be idle
-  int64_t want = (room_for < fill ? room_for : fill) / a.groups;
-  if (want == 0 || 5 * want * a.groups < 4 * (room_for < fill ? room_for : fill)) ++want;
-  a.chunks = want < most ? want : most;
+  int64_t want = fill / a.groups;
+  if (5 * want * a.groups < 4 * fill) ++want;
+  return std::min(std::max<int64_t>(want, 1), most);
 }
 
 // Rows past the caches' replacement: of whole lines, where the tensor is too large to be found there again.
@@ -603,13 +609,14 @@ void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s) {
   dt == STRATA_BF16 ? row_norm::run<true>(a, false, s) : row_norm::run<false>(a, false, s);
 }
 
-size_t residual_norm_partial_bytes(NormArgs a) {
-  row_norm::plan_bwd(a);
-  return a.chunks == 1 ? 0 : (size_t)(3 * a.groups * a.chunks * a.width) * sizeof(float);
+size_t residual_norm_partial_bytes(const NormArgs& a, strata_dtype dt) {
+  const bool bf16 = dt == STRATA_BF16;
+  const int64_t chunks = std::max(row_norm::chunks_of(a, bf16, false), row_norm::chunks_of(a, bf16, true));
+  return chunks == 1 ? 0 : (size_t)(3 * a.groups * chunks * a.width) * sizeof(float);
 }
 
 void launch_residual_norm_bwd(NormArgs a, strata_dtype dt, hipStream_t s) {
-  row_norm::plan_bwd(a);
+  a.chunks = row_norm::chunks_of(a, dt == STRATA_BF16, a.gate || a.dshift);
   dt == STRATA_BF16 ? row_norm::run<true>(a, true, s) : row_norm::run<false>(a, true, s);
   const unsigned vectors = !!a.dgate + !!a.dscale + !!a.dshift;
   if (a.chunks == 1 || !vectors) return;

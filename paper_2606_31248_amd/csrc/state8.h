@@ -45,19 +45,22 @@ constexpr uint32_t kBits = 1032u;  // of 8 = 2^3: (127 + 3) << 3, less the code 
 template <bool SECOND>
 __device__ __forceinline__ float decode(uint32_t byte, float unit) {
   const uint32_t c = SECOND ? byte : byte & 127u;
-  const float v = (c < 8u ? (float)c : __uint_as_float((c + kBits) << 20)) * unit;
+  const float low = (float)c, high = __uint_as_float((c + kBits) << 20);
+  const float v = (c < 8u ? low : high) * unit;
   return SECOND ? v : __uint_as_float(__float_as_uint(v) | (byte & 128u) << 24);
 }
 
 // Rounded up where `random`, 16 bits, reaches over the border: the mean over the random
-// numbers is x.  A second moment above 0 keeps code 1: it is divided by.
+// numbers is x.  A second moment above 0 keeps code 1: it is divided by.  Without branches:
+// the code of the part below 8 and that of the part above, one of which is 8.
 template <bool SECOND>
 __device__ __forceinline__ uint32_t encode(float x, float per_unit, uint32_t random) {
   const float t = fabsf(x) * per_unit;
-  const uint32_t small = (uint32_t)(t + (float)random * 0x1p-16f);
-  uint32_t c = t < 8.f ? small : ((__float_as_uint(t) + (random << 4)) >> 20) - kBits;
-  if (SECOND) return x > 0.f && c == 0u ? 1u : c;
-  return c | (x < 0.f ? 128u : 0u);
+  const uint32_t low = (uint32_t)(fminf(t, 8.f) + (float)random * 0x1p-16f);
+  const uint32_t high = (__float_as_uint(fmaxf(t, 8.f)) + (random << 4)) >> 20;
+  const uint32_t c = low + high - (kBits + 8u);
+  if (SECOND) return umax(c, x > 0.f ? 1u : 0u);
+  return c | (__float_as_uint(x) >> 24 & 128u);
 }
 
 // 32 bits of (seed, element): two rounds of a product and a shift, which move every bit.

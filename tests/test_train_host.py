@@ -105,13 +105,13 @@ def test_table_of_a_list():
     e = entries((a, a + 0x40000, a + 0x80000, 4097, BF16), (a + 0x10000, None, None, 33, F32),
                 (a + 0x20000, a + 0x50000, None, 1, F32), (None, None, None, 0, F32), (a + 0x30000, a + 0x60000, None, 2048, F32))
     st, d, raw = table_of(e)
-    assert st == B.STRATA_OK and d.tensors == 5 and d.chunks == 3 + 0 + 1 + 0 + 1 and d.places == 4128 + 64 + 32 + 0 + 2048
+    assert st == B.STRATA_OK and d.tensors == 5 and d.chunks == 5 + 0 + 1 + 0 + 2 and d.places == 4128 + 64 + 32 + 0 + 2048
     r = np.frombuffer(raw[:5 * 56], np.int64).reshape(5, 7)
     assert r[:, 0].tolist() == [a, a + 0x10000, a + 0x20000, 0, a + 0x30000] and r[:, 3].tolist() == [4097, 33, 1, 0, 2048]
     assert r[:, 1].tolist() == [a + 0x40000, 0, a + 0x50000, 0, a + 0x60000] and r[:, 2].tolist() == [a + 0x80000, 0, 0, 0, 0]
-    assert r[:, 4].tolist() == [0, 4128, 4192, 4224, 4224] and r[:, 5].tolist() == [0, 3, 3, 4, 4]
+    assert r[:, 4].tolist() == [0, 4128, 4192, 4224, 4224] and r[:, 5].tolist() == [0, 5, 5, 6, 6]
     assert r[:, 6].tolist() == [1, 0, 0, 0, 0]
-    assert np.frombuffer(raw[5 * 56:5 * 56 + 20], np.int32).tolist() == [0, 0, 0, 2, 4]
+    assert np.frombuffer(raw[5 * 56:5 * 56 + 32], np.int32).tolist() == [0] * 5 + [2, 4, 4]
 
 
 def test_lists_that_are_refused():
@@ -161,7 +161,7 @@ def test_grad_norm_refusals():
     for kw in (dict(most=0.0), dict(most=-1.0), dict(most=math.nan), dict(norm=None), dict(norm=fake(0x10004)),
                dict(ws=fake(0x10008)), dict(q=None)):
         assert call(**kw) == INVALID, kw
-    assert call(ws=None) == WORKSPACE and call(nbytes=39) == WORKSPACE
+    assert call(ws=None) == WORKSPACE and call(nbytes=7) == WORKSPACE
     assert L.strata_grad_norm_workspace_size(ref(p)) == 256
 
 
