@@ -538,6 +538,22 @@ def _on(dev, stream):
     return stream.cuda_stream
 
 
+def _on_gpu(index, stream):
+    """_on for tensors on GPU `index`."""
+    if stream is None and _raw_stream is not None and _current_device() == index:
+        return _raw_stream(index)
+    return _on(torch.device("cuda", index), stream)
+
+
+def _workspace_at(t, index):
+    """(address, bytes) of a workspace on GPU `index`, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if not (type(t) is torch.Tensor and t.get_device() == index and t.is_contiguous()):
+        _need("workspace", t, device=torch.device("cuda", index))
+    return t.data_ptr(), t.nbytes
+
+
 def _at(name: str, t, shape, dtype, device):
     """The address of a tensor of exactly this shape, dtype and device, or None for None: one pass over the
     conditions, and _need for the message where one fails."""
@@ -649,50 +665,48 @@ def make_norm_desc(rows, group_rows: Optional[int] = None, eps: float = 1e-6) ->
     return NormDesc(many, many if group_rows is None else group_rows, width, float(eps), _dtype(rows))
 
 
-def _norm_at(desc: NormDesc, dev, dt, **tensors):
-    """Addresses of tensors of rows * width elements of dtype `dt` on `dev`, None for None."""
-    n, width = desc.rows * desc.width, desc.width
-    out = []
-    for name, t in tensors.items():
-        if t is None:
-            out.append(None)
-            continue
-        if not (type(t) is torch.Tensor and t.dtype is dt and t.device == dev and t.is_contiguous() and t.numel() == n
-                and t.shape[-1] == width):
-            _need(name, t, None, dt, dev)
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {desc.rows} rows of {width}")
-        out.append(t.data_ptr())
-    return out
+def _rows_at(name, t, n, width, dt, index):
+    """The address of a tensor of n elements in rows of `width`, of dtype `dt` on GPU `index`; None for None."""
+    if t is None:
+        return None
+    if not (type(t) is torch.Tensor and t.dtype is dt and t.get_device() == index and t.is_contiguous() and t.numel() == n
+            and t.shape[-1] == width):
+        _need(name, t, None, dt, torch.device("cuda", index))
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {n // max(width, 1)} rows of {width}")
+    return t.data_ptr()
 
 
-def _vectors_at(desc: NormDesc, dev, **vectors):
-    """Addresses of float32 [groups, width] ([width] for a single group), None for None."""
-    groups, width = desc.rows // max(desc.group_rows, 1), desc.width
-    return [None if t is None else
-            _at(name, t, (width,) if groups == 1 and getattr(t, "ndim", 0) == 1 else (groups, width), torch.float32, dev)
-            for name, t in vectors.items()]
+def _vector_at(name, t, groups, width, index):
+    """The same for float32 [groups, width] ([width] for a single group)."""
+    if t is None:
+        return None
+    if not (type(t) is torch.Tensor and t.dtype is torch.float32 and t.get_device() == index and t.is_contiguous()
+            and (t.shape == (groups, width) or groups == 1 and t.shape == (width,))):
+        _need(name, t, (groups, width), torch.float32, torch.device("cuda", index))
+    return t.data_ptr()
 
 
 def _norm_common(desc: NormDesc, name, t):
-    dt = _torch_dtype(desc.dtype)
-    if not (type(t) is torch.Tensor and t.is_cuda and t.dtype is dt):
+    """(elements, rows' width, groups, dtype, GPU of `t`)"""
+    dt, width, rows, per = _torch_dtype(desc.dtype), desc.width, desc.rows, desc.group_rows
+    if not (type(t) is torch.Tensor and t.is_cuda):
         _need(name, t, None, dt)
-    return dt, t.device
+    return rows * width, width, rows // per if per > 0 else 0, dt, t.get_device()
 
 
 def strata_residual_norm(desc: NormDesc, x, gate, res, scale, shift, sum, y=None, codes=None, scales=None, stream=None):
     """sum = res + gate x, y = its RMS norm with scale and shift, and / or y in 8 bits (codes int8 of y's shape,
     scales uint8 of a 32nd of its elements).  Without x (gate and sum None) the norm of res."""
-    dt, dev = _norm_common(desc, "res", res)
-    px, pres, psum, py = _norm_at(desc, dev, dt, x=x, res=res, sum=sum, y=y)
-    pcodes, = _norm_at(desc, dev, torch.int8, codes=codes)
+    n, w, groups, dt, i = _norm_common(desc, "res", res)
     if scales is not None:
-        _need("scales", scales, None, torch.uint8, dev)
-        if scales.numel() != desc.rows * desc.width // 32:
-            raise ValueError(f"scales: {scales.numel()} elements, expected {desc.rows * desc.width // 32}")
-    pgate, pscale, pshift = _vectors_at(desc, dev, gate=gate, scale=scale, shift=shift)
-    _check(load().strata_residual_norm(ctypes.byref(desc), px, pgate, pres, pscale, pshift, psum, py, pcodes, _ptr(scales),
-                                       _on(dev, stream)))
+        _need("scales", scales, None, torch.uint8, res.device)
+        if scales.numel() != n // 32:
+            raise ValueError(f"scales: {scales.numel()} elements, expected {n // 32}")
+    _check(load().strata_residual_norm(
+        ctypes.byref(desc), _rows_at("x", x, n, w, dt, i), _vector_at("gate", gate, groups, w, i),
+        _rows_at("res", res, n, w, dt, i), _vector_at("scale", scale, groups, w, i), _vector_at("shift", shift, groups, w, i),
+        _rows_at("sum", sum, n, w, dt, i), _rows_at("y", y, n, w, dt, i), _rows_at("codes", codes, n, w, torch.int8, i),
+        None if scales is None else scales.data_ptr(), _on_gpu(i, stream)))
 
 
 def strata_residual_norm_bwd_workspace_size(desc: NormDesc) -> int:
@@ -702,14 +716,14 @@ def strata_residual_norm_bwd_workspace_size(desc: NormDesc) -> int:
 def strata_residual_norm_bwd(desc: NormDesc, sum, x, gate, scale, dy, dsum, dres, dx=None, dgate=None, dscale=None,
                              dshift=None, workspace=None, stream=None):
     """Gradients dres (and dx, with a gate) of the rows and dgate, dscale, dshift of the vectors for dy and dsum."""
-    dt, dev = _norm_common(desc, "sum", sum)
-    psum, px, pdy, pdsum, pdres, pdx = _norm_at(desc, dev, dt, sum=sum, x=x, dy=dy, dsum=dsum, dres=dres, dx=dx)
-    pgate, pscale, pdgate, pdscale, pdshift = _vectors_at(desc, dev, gate=gate, scale=scale, dgate=dgate, dscale=dscale,
-                                                          dshift=dshift)
-    _need("workspace", workspace, device=dev, optional=True)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().strata_residual_norm_bwd(ctypes.byref(desc), psum, px, pgate, pscale, pdy, pdsum, pdres, pdx, pdgate,
-                                           pdscale, pdshift, _ptr(workspace), nbytes, _on(dev, stream)))
+    n, w, groups, dt, i = _norm_common(desc, "sum", sum)
+    at, nbytes = _workspace_at(workspace, i)
+    _check(load().strata_residual_norm_bwd(
+        ctypes.byref(desc), _rows_at("sum", sum, n, w, dt, i), _rows_at("x", x, n, w, dt, i),
+        _vector_at("gate", gate, groups, w, i), _vector_at("scale", scale, groups, w, i), _rows_at("dy", dy, n, w, dt, i),
+        _rows_at("dsum", dsum, n, w, dt, i), _rows_at("dres", dres, n, w, dt, i), _rows_at("dx", dx, n, w, dt, i),
+        _vector_at("dgate", dgate, groups, w, i), _vector_at("dscale", dscale, groups, w, i),
+        _vector_at("dshift", dshift, groups, w, i), at, nbytes, _on_gpu(i, stream)))
 
 
 class Params:
@@ -717,11 +731,8 @@ class Params:
     at: the first of each tensor's."""
 
     def __init__(self, tensors, desc, table, at, device):
-        self.tensors, self.desc, self.table, self.at, self.device = tensors, desc, table, at, device  # tensors: kept alive
-
-    @property
-    def places(self) -> int:
-        return self.desc.places
+        self.tensors, self.desc, self.table, self.at = tensors, desc, table, at  # tensors: kept alive
+        self.device, self.index, self.places = device, device.index, desc.places
 
 
 def make_params(p, g, copies=None) -> Params:
@@ -732,21 +743,26 @@ def make_params(p, g, copies=None) -> Params:
     copies = [None] * len(p) if copies is None else list(copies)
     if not p or len(g) != len(p) or len(copies) != len(p):
         raise ValueError(f"make_params: {len(p)} weights, {len(g)} gradients, {len(copies)} copies")
-    dev, entries, at, place = None, (ParamEntry * len(p))(), [], 0
+    entries, at, place, index = [], [], 0, p[0].get_device() if isinstance(p[0], torch.Tensor) else -1
+    f32, bf16, tensors = torch.float32, torch.bfloat16, (torch.Tensor, torch.nn.Parameter)
     for i, (w, d, c) in enumerate(zip(p, g, copies)):
-        _need(f"p[{i}]", w, None, torch.float32, dev)
-        dev = w.device
+        if not (type(w) in tensors and w.dtype is f32 and w.get_device() == index >= 0 and w.is_contiguous()):
+            _need(f"p[{i}]", w, None, f32, None if index < 0 else torch.device("cuda", index))
+        kind = STRATA_F32
         if d is not None:
-            _need(f"g[{i}]", d, w.shape, None, dev)
-            _dtype(d)
-        if c is not None:
-            _need(f"copies[{i}]", c, w.shape, torch.bfloat16, dev)
+            kind = STRATA_BF16 if type(d) in tensors and d.dtype is bf16 else STRATA_F32
+            if not (type(d) in tensors and (kind == STRATA_BF16 or d.dtype is f32) and d.get_device() == index
+                    and d.shape == w.shape and d.is_contiguous()):
+                _need(f"g[{i}]", d, w.shape, f32, w.device)
+        if c is not None and not (type(c) in tensors and c.dtype is bf16 and c.get_device() == index
+                                  and c.shape == w.shape and c.is_contiguous()):
+            _need(f"copies[{i}]", c, w.shape, bf16, w.device)
         n = w.numel()
-        entries[i] = ParamEntry(w.data_ptr() if n else None, None if d is None or not n else d.data_ptr(),
-                                None if c is None or not n else c.data_ptr(), n,
-                                STRATA_F32 if d is None else _dtype(d))
+        entries.append((w.data_ptr() or None, None if d is None else d.data_ptr() or None,
+                        None if c is None else c.data_ptr() or None, n, kind))
         at.append(place)
         place += (n + 31) // 32 * 32
+    dev, entries = p[0].device, (ParamEntry * len(p))(*entries)
     nbytes, desc = int(load().strata_params_bytes(entries, len(p))), ParamList()
     table = torch.empty(max(nbytes, 1), dtype=torch.uint8)
     _check(load().strata_params_table(entries, len(p), table.data_ptr(), nbytes, ctypes.byref(desc)))
@@ -761,11 +777,9 @@ def strata_grad_norm_workspace_size(params: Params) -> int:
 
 def strata_grad_norm(params: Params, max_norm, norm, workspace, stream=None):
     """norm (float32 [2]): the norm of all gradients and the factor that brings it to max_norm at most."""
-    dev = params.device
-    at = _at("norm", norm, (2,), torch.float32, dev)
-    _need("workspace", workspace, device=dev, optional=True)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().strata_grad_norm(ctypes.byref(params.desc), max_norm, at, _ptr(workspace), nbytes, _on(dev, stream)))
+    i = params.index
+    at, (ws, nbytes) = _vector_at("norm", norm, 1, 2, i), _workspace_at(workspace, i)
+    _check(load().strata_grad_norm(ctypes.byref(params.desc), max_norm, at, ws, nbytes, _on_gpu(i, stream)))
 
 
 def make_adamw_desc(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0) -> AdamWDesc:
@@ -773,19 +787,25 @@ def make_adamw_desc(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0
     return AdamWDesc(lr, beta1, beta2, eps, weight_decay, step, seed % (1 << 64))
 
 
+def _flat_at(name, t, n, dt, index):
+    """The address of a tensor [n] of dtype `dt` on GPU `index`."""
+    if not (type(t) is torch.Tensor and t.dtype is dt and t.get_device() == index and t.shape == (n,) and t.is_contiguous()):
+        _need(name, t, (n,), dt, torch.device("cuda", index))
+    return t.data_ptr() or None
+
+
 def strata_adamw(desc: AdamWDesc, params: Params, m, v, m_scales=None, v_scales=None, factor=None, stream=None):
     """One step on every tensor of the list that has a gradient.  m, v: float32 [places], or uint8 with scales
     uint8 [places / 32]; factor: float32 [1], what the gradients are multiplied by (NaN: nothing is changed)."""
-    dev, n = params.device, params.places
-    eight = m_scales is not None or v_scales is not None
-    dt = torch.uint8 if eight else torch.float32
-    for name, t in (("m", m), ("v", v)) + ((("m_scales", m_scales), ("v_scales", v_scales)) if eight else ()):
-        _like(name, t, (n // 32,) if name.endswith("scales") else (n,), dt, dev)
-    if factor is not None:
-        _like("factor", factor, (1,), torch.float32, dev)
-    at = [None if t is None or not n else t.data_ptr() for t in (m, v, m_scales, v_scales)]
-    _check(load().strata_adamw(ctypes.byref(desc), ctypes.byref(params.desc), *at,
-                               None if factor is None else factor.data_ptr(), _on(dev, stream)))
+    i, n = params.index, params.places
+    if m_scales is None and v_scales is None:
+        at = (_flat_at("m", m, n, torch.float32, i), _flat_at("v", v, n, torch.float32, i), None, None)
+    else:
+        u8 = torch.uint8
+        at = (_flat_at("m", m, n, u8, i), _flat_at("v", v, n, u8, i), _flat_at("m_scales", m_scales, n // 32, u8, i),
+              _flat_at("v_scales", v_scales, n // 32, u8, i))
+    f = None if factor is None else _flat_at("factor", factor, 1, torch.float32, i)
+    _check(load().strata_adamw(ctypes.byref(desc), ctypes.byref(params.desc), *at, f, _on_gpu(i, stream)))
 
 
 def strata_adamw_unpack(codes, scales, values, second, stream=None):
@@ -794,8 +814,9 @@ def strata_adamw_unpack(codes, scales, values, second, stream=None):
         _need("values", values)
     n, dev = values.numel(), values.device
     for name, t, many in (("codes", codes, n), ("scales", scales, (n + 31) // 32)):
-        _need(name, t, None, torch.uint8, dev)
-        if t.numel() != many:
+        if not (type(t) is torch.Tensor and t.dtype is torch.uint8 and t.device == dev and t.numel() == many
+                and t.is_contiguous()):
+            _need(name, t, None, torch.uint8, dev)
             raise ValueError(f"{name}: {t.numel()} elements, expected {many}")
     _check(load().strata_adamw_unpack(codes.data_ptr(), scales.data_ptr(), n, int(bool(second)), values.data_ptr(),
                                       _dtype(values), _on(dev, stream)))

@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double* partial, i
   norm[1] = !(x <= 0x1.fffffffffffffp1023) ? __uint_as_float(0x7FC00000u) : x <= most ? 1.f : (float)(most / x);
 }
 
-constexpr int kNormBlocks = 1024;
+constexpr int kNormBlocks = 2048;
 
 }  // namespace adamw
 

@@ -317,6 +317,14 @@ def test_streams_and_replays():
                     w.g[i].copy_(torch.randn(tuple(g.shape), generator=gen(50 + k)) * 1e-3)
 
 
+def test_parameters_of_a_module():
+    """nn.Parameter weights and copies are updated like plain tensors."""
+    a, b = Weights([(5, 7), 300], "f32"), Weights([(5, 7), 300], "f32")
+    b.list = B.make_params([torch.nn.Parameter(p) for p in b.p], b.g, [torch.nn.Parameter(c) for c in b.copies])
+    a.step(), b.step()
+    assert all(torch.equal(x, y) for x, y in zip(a.p + a.copies + [a.m, a.v], b.p + b.copies + [b.m, b.v]))
+
+
 def test_beyond_32_bit_offsets():
     """32-bit states of two tensors of 2^31 + 100 weights each: the second lies behind place 2^31."""
     n = (1 << 31) + 100
