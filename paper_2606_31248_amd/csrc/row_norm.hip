@@ -455,15 +455,17 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) bwd_kern
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       float(&d)[8] = which == 0 ? dgate[ALL ? i : 0] : which == 1 ? dscale[i] : dshift[ALL ? i : 0];
+      if (BLOCK) {
+        Piece<false> p;
+        p.set(d);
+        p.template store<LIE == kLines ? kWhole : LIE>(out, at.first + i * at.step, at.gap, n[i]);
+        continue;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int c = at.first + i * at.step + (j < 4 ? j : at.gap + j - 4);
-        if (BLOCK) {
-          if (c < width) out[c] = d[j];
-        } else {
-          const float x = teams_sum<LANES>(d[j]);
-          if ((threadIdx.x & 63) < LANES) wide[threadIdx.x >> 6][c] = x;
-        }
+        const float x = teams_sum<LANES>(d[j]);
+        if ((threadIdx.x & 63) < LANES)
+          wide[threadIdx.x >> 6][at.first + i * at.step + (j < 4 ? j : at.gap + j - 4)] = x;
       }
     }
     if (BLOCK) continue;
