@@ -4,7 +4,9 @@ One rollout pass: coordinates (Eq. 1) -> StereoRoPE phases -> neighbourhood
 attention forward with the rotation fused into the Q/K loads -> tile stitch
 S = D^-1 P^T W.  One training block, from its projection's rows to their gradient:
 ``block_forward`` and ``block_backward``, with the rows and the attention's output
-kept between them as they are or in 8 bits.
+kept between them as they are or in 8 bits.  Around the blocks: the residual stream's
+addition with its norm (``norm_forward``, ``norm_backward``), and the update of all weights
+from their gradients (``AdamW``).
 PyTorch only allocates device memory and supplies the stream.
 """
 from __future__ import annotations
@@ -164,6 +166,103 @@ def block_backward(saved: BlockSaved, dout):
     B.strata_qkv_heads_bwd(d, rows, codes, scales, saved.wq, saved.wk, saved.cs, dq, dk, dv, dgate, drows, dwq, dwk,
                            ws)
     return drows, dwq, dwk
+
+
+@dataclasses.dataclass
+class NormSaved:
+    """What the entry of a block keeps: the stream (res itself without a branch), the branch that was added where it
+    has a gate, the vectors, and the norm's output, as it is or as (codes, scales), for the weights' gradient of the
+    projection that read it."""
+    desc: B.NormDesc
+    total: torch.Tensor
+    x: Optional[torch.Tensor]
+    gate: Optional[torch.Tensor]
+    scale: Optional[torch.Tensor]
+    shift: Optional[torch.Tensor]
+    held: object
+
+    def output(self) -> torch.Tensor:
+        """The norm's output, from 8 bits the values of its codes."""
+        if not isinstance(self.held, tuple):
+            return self.held
+        y = torch.empty_like(self.total)
+        B.strata_ckpt_unpack(*self.held, y)
+        return y
+
+
+def norm_forward(res, x=None, gate=None, scale=None, shift=None, group_rows: Optional[int] = None, eps: float = 1e-6,
+                 eight_bit: bool = False):
+    """Entry of a block: (y, sum, saved), sum = res + gate x (res itself without x) and y = scale rms(sum) + shift.
+
+    res, x: [..., width]; gate, scale, shift: float32 [groups, width] or None, one for every group_rows consecutive
+    rows (default: one for all).  eight_bit: `saved` holds y in 8 bits, for a width of whole 32."""
+    desc = B.make_norm_desc(res, group_rows, eps)
+    total = res if x is None else torch.empty_like(res)
+    y = torch.empty_like(res)
+    codes = scales = None
+    if eight_bit:
+        codes = torch.empty(res.shape, dtype=torch.int8, device=res.device)
+        scales = torch.empty(res.shape[:-1] + (res.shape[-1] // 32,), dtype=torch.uint8, device=res.device)
+    B.strata_residual_norm(desc, x, gate, res, scale, shift, None if x is None else total, y, codes, scales)
+    return y, total, NormSaved(desc, total, None if gate is None else x, gate, scale, shift, (codes, scales) if eight_bit else y)
+
+
+def norm_backward(saved: NormSaved, dy, dsum=None):
+    """Gradients of norm_forward for those of y and of sum (None: 0): (dres, dx, dgate, dscale, dshift).
+
+    dx is dres itself without a gate; None for a vector that was None."""
+    dres = torch.empty_like(dy)
+    dx, dgate = (None, None) if saved.gate is None else (torch.empty_like(dy), torch.empty_like(saved.gate))
+    dscale, dshift = (None if v is None else torch.empty_like(v) for v in (saved.scale, saved.shift))
+    ws = torch.empty(B.strata_residual_norm_bwd_workspace_size(saved.desc), dtype=torch.uint8, device=dy.device)
+    B.strata_residual_norm_bwd(saved.desc, saved.total, saved.x, saved.gate, saved.scale, dy, dsum, dres, dx, dgate, dscale,
+                               dshift, ws)
+    return dres, dres if dx is None else dx, dgate, dscale, dshift
+
+
+class AdamW:
+    """AdamW over a list of weights, with the norm of their gradients clipped and the states in 32 bits or in 8.
+
+    p, g, copies: as binding.make_params takes them; the tensors stay where they are.  m, v and, in 8 bits, m_scales
+    and v_scales are the states, flat, and `steps` the steps taken: what a checkpoint stores.  A step whose gradients
+    are not all finite changes no tensor if it clips (max_norm, which may be infinity), but is counted."""
+
+    def __init__(self, p, g, copies=None, eight_bit: bool = False, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, weight_decay: float = 0.0, max_norm: Optional[float] = None, seed: int = 0):
+        self.params = B.make_params(p, g, copies)
+        self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
+        self.max_norm, self.seed, self.steps = max_norm, seed, 0
+        n, dev = self.params.places, self.params.device
+        self.m, self.v = (torch.zeros(n, dtype=torch.uint8 if eight_bit else torch.float32, device=dev) for _ in range(2))
+        self.m_scales, self.v_scales = ((torch.zeros(n // 32, dtype=torch.uint8, device=dev) for _ in range(2)) if eight_bit
+                                        else (None, None))
+        self._norm = torch.empty(2, dtype=torch.float32, device=dev)
+        self._ws = torch.empty(B.strata_grad_norm_workspace_size(self.params), dtype=torch.uint8, device=dev)
+
+    def step(self, lr: float) -> Optional[torch.Tensor]:
+        """One step from the gradients that are in place.  With max_norm: float32 [2] on the device, the gradients'
+        norm and the factor they were multiplied by, overwritten by the next step."""
+        self.steps += 1
+        norm = None
+        if self.max_norm is not None:
+            norm = self._norm
+            B.strata_grad_norm(self.params, self.max_norm, norm, self._ws)
+        desc = B.make_adamw_desc(lr, self.steps, seed=(self.seed << 40) + self.steps, **self.hyper)
+        B.strata_adamw(desc, self.params, self.m, self.v, self.m_scales, self.v_scales, None if norm is None else norm[1:])
+        return norm
+
+    def moments(self, i: int):
+        """(m, v) of tensor i as float32 tensors of its shape."""
+        w = self.params.tensors[0][i]
+        at, n = self.params.at[i], w.numel()
+        cut = lambda t, k=1: t[at // k:at // k + -(-n // k)]  # noqa: E731
+        if self.m_scales is None:
+            return cut(self.m).clone().view(w.shape), cut(self.v).clone().view(w.shape)
+        m, v = (torch.empty(w.shape, dtype=torch.float32, device=w.device) for _ in range(2))
+        if n:
+            B.strata_adamw_unpack(cut(self.m), cut(self.m_scales, 32).clone(), m, second=False)
+            B.strata_adamw_unpack(cut(self.v), cut(self.v_scales, 32).clone(), v, second=True)
+        return m, v
 
 
 def face_step(q, k, v, geom: TileGeometry, window, scale, tiling, blend_window, face_out,

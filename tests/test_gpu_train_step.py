@@ -1,0 +1,194 @@
+"""A training step of the pieces together: the stream's norm, a projection, the attention block, the projection behind
+it, the next norm, all gradients, their norm and AdamW (pipeline.norm_forward, block_forward, block_backward,
+norm_backward, AdamW)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train as T
+from paper_2606_31248_amd import binding as B
+from paper_2606_31248_amd import pipeline
+
+from _rows import TYPE, f64, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+GRID, HEADS, D, WIDTH, WINDOW = (2, 3, 5, 6), 2, 32, 64, (3, 3, 5)   # B, Z, H, W; two tiles
+TOKENS, PER = 180, 90
+HYPER = dict(beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.01)
+NAMES = ("wqkv", "wo", "gate0", "scale0", "shift0", "scale1", "wq", "wk")
+
+
+class Step:
+    """Weights, inputs and upstream gradients; the projections are torch products in the activations' type."""
+
+    def __init__(self, dtype, eight=False, seed=0):
+        g = gen(seed + 70)
+        t = TYPE[dtype]
+        self.dtype, self.eight = dtype, eight
+        self.qkv = B.make_qkv_desc(*(GRID[0], HEADS) + GRID[1:], D, B.STRATA_BF16 if dtype == "bf16" else B.STRATA_F32, gate_dim=1)
+        rand = lambda *s, mult=1.0, mean=0.0: (mean + mult * torch.randn(s, generator=g)).cuda()  # noqa: E731
+        self.w = dict(wqkv=rand(self.qkv.width, WIDTH, mult=WIDTH ** -0.5), wo=rand(WIDTH, HEADS * D, mult=(HEADS * D) ** -0.5),
+                      gate0=rand(2, WIDTH, mult=0.2, mean=0.5), scale0=rand(2, WIDTH, mult=0.2, mean=1.0),
+                      shift0=rand(2, WIDTH, mult=0.2), scale1=rand(1, WIDTH, mult=0.2, mean=1.0),
+                      wq=rand(D, mult=0.2, mean=1.0), wk=rand(D, mult=0.2, mean=1.0))
+        self.copies = {n: w.to(t) for n, w in self.w.items()} if dtype == "bf16" else {}
+        self.g = {n: torch.zeros_like(w) for n, w in self.w.items()}
+        self.inputs = {n: normal((TOKENS, WIDTH), dtype, g) for n in ("s0", "x0", "dy", "dsum")}
+
+    def weight(self, n):
+        return self.copies.get(n, self.w[n])
+
+    def run(self):
+        """Forward and backward; the gradients into self.g.  (y1, s2, ds0, dx0)"""
+        i, w, q = self.inputs, self.w, self.qkv
+        y0, s1, n0 = pipeline.norm_forward(i["s0"], i["x0"], w["gate0"], w["scale0"], w["shift0"], group_rows=PER, eight_bit=self.eight)
+        rows = torch.zeros(GRID + (q.row_stride,), dtype=y0.dtype, device="cuda")
+        rows.view(TOKENS, -1)[:, :q.width] = y0 @ self.weight("wqkv").t()
+        out, saved = pipeline.block_forward(rows, q, WINDOW, D ** -0.5, w["wq"], w["wk"], eight_bit=self.eight)
+        flat = out.permute(0, 2, 3, 4, 1, 5).reshape(TOKENS, HEADS * D)
+        y1, s2, n1 = pipeline.norm_forward(s1, flat @ self.weight("wo").t(), scale=w["scale1"])
+        ds1, dx1, _, dscale1, _ = pipeline.norm_backward(n1, i["dy"], i["dsum"])
+        dout = (dx1 @ self.weight("wo")).view(GRID + (HEADS, D)).permute(0, 4, 1, 2, 3, 5).contiguous()
+        drows, dwq, dwk = pipeline.block_backward(saved, dout)
+        drows = drows.view(TOKENS, -1)[:, :q.width].contiguous()
+        ds0, dx0, dgate0, dscale0, dshift0 = pipeline.norm_backward(n0, drows @ self.weight("wqkv"), ds1)
+        new = dict(wqkv=drows.t() @ n0.output(), wo=dx1.t() @ flat, gate0=dgate0, scale0=dscale0, shift0=dshift0,
+                   scale1=dscale1, wq=dwq, wk=dwk)
+        for n, g in new.items():
+            self.g[n].copy_(g)
+        return y1, s2, ds0, dx0
+
+    def optimiser(self, **kw):
+        return pipeline.AdamW([self.w[n] for n in NAMES], [self.g[n] for n in NAMES],
+                              [self.copies.get(n) for n in NAMES], **dict(HYPER, **kw))
+
+
+def attend64(q, k, v, gate):
+    """Neighbourhood attention in torch float64, [B, heads, Z, H, W, d], by a mask over all pairs of tokens."""
+    near = []
+    for size, win in zip(GRID[1:], WINDOW):
+        start = (torch.arange(size) - win // 2).clamp(0, size - win)[:, None]
+        at = torch.arange(size)[None]
+        near.append((at >= start) & (at < start + win))
+    z, h, w = near
+    mask = (z[:, None, None, :, None, None] & h[None, :, None, None, :, None] & w[None, None, :, None, None, :]).reshape(PER, PER)
+    flat = lambda x: x.reshape(GRID[0] * HEADS, PER, D)  # noqa: E731
+    a = torch.bmm(flat(q), flat(k).transpose(1, 2).contiguous()) * D ** -0.5
+    a = torch.softmax(a.masked_fill(~mask, -torch.inf), -1)
+    return torch.bmm(a, flat(v)).view(q.shape) * torch.sigmoid(gate)[..., None]
+
+
+def step64(s):
+    """Values and gradients of Step.run's chain by autograd in float64 on the host."""
+    w = {n: t.cpu().double().requires_grad_() for n, t in s.w.items()}
+    i = {n: t.cpu().double().requires_grad_() for n, t in s.inputs.items()}
+    rms = lambda x: x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()  # noqa: E731
+    wide = lambda v: v.repeat_interleave(PER, 0)  # noqa: E731
+    s1 = i["s0"] + wide(w["gate0"]) * i["x0"]
+    y0 = rms(s1) * wide(w["scale0"]) + wide(w["shift0"])
+    rows = (y0 @ w["wqkv"].t()).view(GRID + (-1,))
+    q, k, v = (rows[..., j * HEADS * D:(j + 1) * HEADS * D].view(GRID + (HEADS, D)).permute(0, 4, 1, 2, 3, 5) for j in range(3))
+    gate = rows[..., 3 * HEADS * D:].permute(0, 4, 1, 2, 3)
+    out = attend64(rms(q) * w["wq"], rms(k) * w["wk"], v, gate)
+    x1 = out.permute(0, 2, 3, 4, 1, 5).reshape(TOKENS, -1) @ w["wo"].t()
+    s2 = s1 + x1
+    y1 = rms(s2) * w["scale1"]
+    (y1 * i["dy"].detach()).sum().add((s2 * i["dsum"].detach()).sum()).backward()
+    return (y1, s2, i["s0"].grad, i["x0"].grad), {n: t.grad for n, t in w.items()}
+
+
+def off(a, b):
+    return float((a.cpu().double() - b).norm() / b.norm())
+
+
+def test_gradients():
+    """float32 against 64 bits.  Nine stages (two norms, two projections, the rows' pass and the attention, forward and
+    back), each within 1e-5 of its outputs' size (the library's rule in float32) and passing errors on by Jacobians of
+    order one: 2e-4 in the 2-norm, twice their sum."""
+    s = Step("f32")
+    got = s.run()
+    want, grads = step64(s)
+    for name, a, b in zip(("y1", "s2", "ds0", "dx0"), got, want):
+        assert off(a, b.detach()) < 2e-4, name
+    for n in NAMES:
+        assert off(s.g[n], grads[n]) < 2e-4, n
+
+
+def test_eight_bits():
+    """bf16: the norm's output, the rows and the attention's output kept in 8 bits move the gradients by the 0.9 % of
+    each code's rounding, the block's by twice that in its logits: under 6 % together; what comes before them not at all."""
+    a, b = Step("bf16"), Step("bf16", eight=True)
+    got, eight = a.run(), b.run()
+    assert torch.equal(got[0], eight[0]) and torch.equal(got[1], eight[1])      # the forward
+    for n in ("wo", "scale1"):
+        assert torch.equal(a.g[n], b.g[n]), n
+    for n in NAMES:
+        assert off(b.g[n], a.g[n].cpu().double()) < 0.06, n
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_update(eight):
+    """The gradients' norm over all tensors and the step it clips, against the oracle; moments of each tensor."""
+    s = Step("bf16")
+    opt = s.optimiser(eight_bit=eight, max_norm=1.0, seed=9)
+    for k in range(1, 4):
+        s.inputs["dy"].copy_(normal((TOKENS, WIDTH), "bf16", gen(k)))
+        s.run()
+        before = {n: f64(s.w[n]) for n in NAMES}
+        moments = [[f64(t) for t in opt.moments(j)] for j in range(len(NAMES))]
+        norm = f64(opt.step(1e-3))
+        total = np.sqrt(sum((f64(g) ** 2).sum() for g in s.g.values()))
+        assert abs(norm[0] - total) <= 2.0 ** -23 * total and total > 1.0 and abs(norm[1] - 1 / total) <= 2.0 ** -23 / total
+        for j, n in enumerate(NAMES):
+            g = f64(s.g[n]) * norm[1]
+            want, m, v = T.adamw(before[n], g, *moments[j], 1e-3, k, HYPER["beta1"], HYPER["beta2"], HYPER["eps"], HYPER["weight_decay"])
+            # an update is below lr / (1 - beta1) here; its float32 arithmetic 2^-19 of that, and one rounding of w
+            assert np.all(np.abs(f64(s.w[n]) - want) <= 2.0 ** -24 * np.abs(want) + 2.0 ** -19 * 1e-2), n
+            assert torch.equal(s.copies[n], s.w[n].bfloat16())
+            got = [f64(t) for t in opt.moments(j)]
+            if not eight:
+                for a, b in zip(got, (m, v)):
+                    assert np.allclose(a, b, rtol=2.0 ** -21, atol=2.0 ** -21 * np.abs(b).max()), n
+            else:   # a code's step is at most 1/8 of the value, or a unit: 2^-17 and 2^-33 octaves below the largest
+                for a, b, u in zip(got, (m, v), (2.0 ** -16, 2.0 ** -32)):
+                    assert np.all(np.abs(a - b) <= np.abs(b) * (1 / 8 + 2.0 ** -20) + u * np.abs(b).max()), n
+
+
+def test_replayed_gradients_and_eager_updates():
+    """Forward and backward captured once and replayed on other inputs, the updates between them eager."""
+    a, b = Step("bf16", eight=True), Step("bf16", eight=True)
+    a.run(), b.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = a.run()
+    opts = [s.optimiser(eight_bit=True, max_norm=0.5) for s in (a, b)]
+    for k in range(3):
+        for s in (a, b):
+            for n, t in s.inputs.items():
+                t.copy_(normal((TOKENS, WIDTH), "bf16", gen(100 * k + len(n))))
+        graph.replay()
+        want = b.run()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+        for o in opts:
+            o.step(1e-3)
+        for n in NAMES:
+            assert torch.equal(a.g[n], b.g[n]) and torch.equal(a.w[n], b.w[n]) and torch.equal(a.copies[n], b.copies[n]), n
+
+
+def test_a_step_of_other_gradients_and_state_size():
+    """Tensors without gradients stay; the states in 8 bits take just over a quarter."""
+    s = Step("f32")
+    s.run()
+    opts = []
+    for eight in (False, True):
+        w = [s.w[n].clone() for n in NAMES]
+        opt = pipeline.AdamW(w, [s.g[n] if n != "wo" else None for n in NAMES], eight_bit=eight, **HYPER)
+        assert opt.step(1e-3) is None
+        assert torch.equal(w[1], s.w["wo"]) and not any(bool(t.any()) for t in opt.moments(1))
+        assert not any(torch.equal(x, s.w[n]) for x, n in zip(w, NAMES) if n != "wo")
+        opts.append(opt)
+    size = lambda o: sum(t.nbytes for t in (o.m, o.v, o.m_scales, o.v_scales) if t is not None)  # noqa: E731
+    assert size(opts[1]) == size(opts[0]) * 33 // 128
