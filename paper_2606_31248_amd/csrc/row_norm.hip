@@ -33,7 +33,9 @@ enum Lie { kLines, kWhole, kRagged };
 // Four elements, 16 bytes of float32, from any address of the type's alignment.  Of a ragged
 // row the lanes at its end load what follows too, which is the next row but behind the last;
 // `keep` clears that where it would count, not here, so that the load stays in flight.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 __attribute__((aligned(4))) float_quad;
+typedef u32x2 __attribute__((aligned(4))) float_pair;
 template <int LIE>
 __device__ __forceinline__ u32x4 load_quad(const float* p, int n, bool inside) {
   u32x4 v = {};
@@ -57,10 +59,9 @@ __device__ __forceinline__ void store_quad(float* p, int n, u32x4 v) {
       store16(p, v);
     else
       *reinterpret_cast<float_quad*>(p) = v;
-  } else if (LIE == kRagged) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[j] = __uint_as_float(v[j]);
+  } else if (LIE == kRagged) {  // 2 and 1: instructions for a lane of a wave cost as much as for all
+    if (n & 2) *reinterpret_cast<float_pair*>(p) = u32x2{v[0], v[1]};
+    if (n & 1) p[n & 2] = __uint_as_float(n & 2 ? v[2] : v[0]);
   }
 }
 
@@ -110,10 +111,12 @@ struct Piece<true> {
         store16(p, a);
       else
         *reinterpret_cast<any*>(p) = a;
-    } else if (LIE == kRagged) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < many) p[j] = (uint16_t)(a[j >> 1] >> (16 * (j & 1)));
+    } else if (LIE == kRagged) {  // 4, 2 and 1
+      typedef u32x2 __attribute__((aligned(2))) four;
+      typedef uint32_t __attribute__((aligned(2))) two;
+      if (many & 4) *reinterpret_cast<four*>(p) = u32x2{a[0], a[1]};
+      if (many & 2) *reinterpret_cast<two*>(p + (many & 4)) = many & 4 ? a[2] : a[0];
+      if (many & 1) p[many & 6] = (uint16_t)(many & 4 ? (many & 2 ? a[3] : a[2]) : many & 2 ? a[1] : a[0]);
     }
   }
 };
