@@ -162,12 +162,12 @@ __device__ __forceinline__ void load_vector(const float* base, int64_t at, int g
 }
 
 // The sum over a team's lanes, in every one of them.
-template <int LANES>  // at least 8
+template <int LANES>
 __device__ __forceinline__ float lanes_sum(float x) {
   auto add = [](float a, uint32_t b) { return a + __uint_as_float(b); };
-  x = add(x, dpp<kSwap1>(__float_as_uint(x)));
-  x = add(x, dpp<kSwap2>(__float_as_uint(x)));
-  x = add(x, dpp<kMirror8>(__float_as_uint(x)));
+  if (LANES >= 2) x = add(x, dpp<kSwap1>(__float_as_uint(x)));
+  if (LANES >= 4) x = add(x, dpp<kSwap2>(__float_as_uint(x)));
+  if (LANES >= 8) x = add(x, dpp<kMirror8>(__float_as_uint(x)));
   if (LANES >= 16) x = add(x, dpp<kMirror16>(__float_as_uint(x)));
   if (LANES >= 32) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -183,8 +183,11 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // The sum over a wave's teams, of the lanes at the same place of each.
 template <int LANES>
 __device__ __forceinline__ float teams_sum(float x) {
-  constexpr int kTurn8 = 0x128;  // row_ror: lanes 8 apart in a row of 16
+  constexpr int kTurn4 = 0x124, kTurn8 = 0x128;  // row_ror: lanes 4, 8 apart in a row of 16
+  if (LANES <= 1) x += __uint_as_float(dpp<kSwap1>(__float_as_uint(x)));
+  if (LANES <= 2) x += __uint_as_float(dpp<kSwap2>(__float_as_uint(x)));
   if (LANES <= 8) x += __uint_as_float(dpp<kTurn8>(__float_as_uint(x)));
+  if (LANES <= 4) x += __uint_as_float(dpp<kTurn4>(__float_as_uint(x)));
   if (LANES <= 16) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -409,30 +412,28 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) bwd_kern
       for (int j = 0; j < 8; ++j) m = fmaf(v[j], v[j], m);
     }
     const float r = rsqrtf(row_sum<LANES, BLOCK>(m, sums, turn) * a.inverse + a.eps);
-    // with y = r s, u = r scale dy: dres = u - y mean(u y) + dsum, r never squared: it may reach 2^74
-    float dot = 0.f;
+    // with y = r s, u = scale dy, m = mean(u y): dres = r (u - y m) + dsum, r never squared: it may reach 2^74
+    float dot = 0.f, y[PIECES][8], u[PIECES][8];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      float v[8], u[8];
-      in.s[i].get(v);
-      in.up[i].get(u);
+      in.s[i].get(y[i]);
+      in.up[i].get(u[i]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dot = fmaf(u[j] * scale[i][j] * r, v[j] * r, dot);
+      for (int j = 0; j < 8; ++j) {
+        y[i][j] *= r;
+        dscale[i][j] = fmaf(u[i][j], y[i][j], dscale[i][j]);
+        if (ALL) dshift[i][j] += u[i][j];
+        u[i][j] *= scale[i][j];
+        dot = fmaf(u[i][j], y[i][j], dot);
+      }
     }
     dot = row_sum<LANES, BLOCK>(dot, sums, turn) * a.inverse;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      float v[8], u[8], h[8];
-      in.s[i].get(v);
-      in.up[i].get(u);
+      float h[8], v[8];
       in.ds[i].get(h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] *= r;
-        dscale[i][j] = fmaf(u[j], v[j], dscale[i][j]);
-        if (ALL) dshift[i][j] += u[j];
-        h[j] += fmaf(-v[j], dot, u[j] * scale[i][j] * r);
-      }
+      for (int j = 0; j < 8; ++j) h[j] = fmaf(r, fmaf(-y[i][j], dot, u[i][j]), h[j]);
       in.s[i].set(h);
       in.s[i].template store<LIE>(a.dres, row + i * at.step, at.gap, n[i]);
       if (ALL && a.x) {
@@ -524,7 +525,7 @@ static Shape shape_of(int width, bool back) {
   // Two pieces a lane in the backward where rows are long enough for 8 lanes: half as many exchanges an element, and a
   // wave has twice as much in flight.  The forward has more waves in flight instead (rows of 512: 6.5 and 6.2 TB/s).
   const int most = width > 64 && back ? 2 : 1;
-  int lanes = 8;
+  int lanes = width % 32 ? 1 : 8;  // 8 lanes hold the float32 values of a group of codes
   while (lanes < 64 && lanes * 8 * most < width) lanes *= 2;
   return {lanes, lanes * 8 < width ? 2 : 1, kWaves * 64, kWaves * 64 / lanes};
 }
@@ -540,7 +541,8 @@ static int64_t fwd_blocks(const NormArgs& a) {
 // many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.8, 5.5; with a
 // gate 5.9, 5.0, 5.4), two where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's
 // two more streams and three sums (rows of 4096 5.9, 5.5, 5.3).  If rows are many, ragged ones two (rows of 201: 4.3,
-// 5.0, 4.8) and gated ones of float32 four (5.2, 5.7, 6.0).
+// 5.0, 4.8) or, short ones with a piece a lane, four (rows of 33: 2.4, 3.2, 4.2), and gated ones of float32 four (5.2,
+// 5.7, 6.0).
 constexpr int kCus = 256;
 static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
   const Shape at = shape_of(a.width, true);
@@ -548,7 +550,7 @@ static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
     const int waves = at.threads / 64, want = all ? 4 : 8;
     return waves >= want ? kCus : kCus * (want / waves);
   }
-  const int want = a.width % 8 ? 2 : all && !bf16 ? 4 : 1;
+  const int want = a.width % 8 ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1;
   return a.rows >= (int64_t)kCus * want * 8 * at.teams ? kCus * want : kCus;
 }
 
@@ -586,6 +588,9 @@ static void run(const NormArgs& a, bool back, hipStream_t s) {
   if (at.teams == 1) return start<BF16, 64, 2, true, LIE>(a, back, at, s);
   if (at.pieces == 1) {
     switch (at.lanes) {
+      case 1: return start<BF16, 1, 1, false, LIE>(a, back, at, s);
+      case 2: return start<BF16, 2, 1, false, LIE>(a, back, at, s);
+      case 4: return start<BF16, 4, 1, false, LIE>(a, back, at, s);
       case 8: return start<BF16, 8, 1, false, LIE>(a, back, at, s);
       case 16: return start<BF16, 16, 1, false, LIE>(a, back, at, s);
       case 32: return start<BF16, 32, 1, false, LIE>(a, back, at, s);
