@@ -249,6 +249,13 @@ __device__ __forceinline__ double block_sum(double x) {
   return sums[0];
 }
 
+// The norm and the factor from the sum of squares.
+__device__ __forceinline__ void store_norm(double squares, double most, float* norm) {
+  const double x = sqrt(squares);
+  norm[0] = (float)x;
+  norm[1] = !(x <= 0x1.fffffffffffffp1023) ? __uint_as_float(0x7FC00000u) : x <= most ? 1.f : (float)(most / x);
+}
+
 __device__ __forceinline__ void add_square(double& x, float v) { x = fma((double)v, (double)v, x); }
 
 // Squares of float32 values in float64: neither range nor digits are lost, whatever the count.
@@ -275,7 +282,7 @@ __device__ __forceinline__ void square_run(const ParamRecord& t, int64_t base, d
 }
 
 __global__ void __launch_bounds__(kThreads) squares_kernel(const ParamRecord* tensors, const int32_t* owner,
-                                                           int64_t chunks, double* partial) {
+                                                           int64_t chunks, double* partial, double most, float* norm) {
   constexpr int kParts = kParamChunk / kSpan, kAll = kRun * kParamChunk;
   double x = 0., y = 0.;
   for (int64_t run = (int64_t)blockIdx.x * kRun; run < chunks; run += (int64_t)gridDim.x * kRun) {
@@ -300,16 +307,18 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const ParamRecord* te
     }
   }
   x = block_sum(x + y);
-  if (threadIdx.x == 0) partial[blockIdx.x] = x;
+  if (threadIdx.x) return;
+  if (gridDim.x == 1)
+    store_norm(x, most, norm);
+  else
+    partial[blockIdx.x] = x;
 }
 
 __global__ void __launch_bounds__(kThreads) norm_kernel(const double* partial, int blocks, double most, float* norm) {
   double x = 0.;
   for (int i = threadIdx.x; i < blocks; i += kThreads) x += partial[i];
-  x = sqrt(block_sum(x));
-  if (threadIdx.x) return;
-  norm[0] = (float)x;
-  norm[1] = !(x <= 0x1.fffffffffffffp1023) ? __uint_as_float(0x7FC00000u) : x <= most ? 1.f : (float)(most / x);
+  x = block_sum(x);
+  if (threadIdx.x == 0) store_norm(x, most, norm);
 }
 
 constexpr int kNormBlocks = 2048;
@@ -345,14 +354,16 @@ void launch_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n,
 
 int64_t grad_norm_blocks(int64_t chunks) {
   const int64_t runs = (chunks + adamw::kRun - 1) / adamw::kRun;
-  return runs < adamw::kNormBlocks ? runs : adamw::kNormBlocks;
+  return runs <= 2 ? chunks > 0 : runs < adamw::kNormBlocks ? runs : adamw::kNormBlocks;  // one block: one launch
 }
 
 void launch_grad_norm(const ParamRecord* tensors, const int32_t* owner, int64_t chunks, double most, float* norm,
                       double* partial, hipStream_t s) {
   const int blocks = (int)grad_norm_blocks(chunks);
   if (blocks)
-    hipLaunchKernelGGL(adamw::squares_kernel, dim3(blocks), dim3(adamw::kThreads), 0, s, tensors, owner, chunks, partial);
+    hipLaunchKernelGGL(adamw::squares_kernel, dim3(blocks), dim3(adamw::kThreads), 0, s, tensors, owner, chunks, partial,
+                       most, norm);
+  if (blocks == 1) return;
   hipLaunchKernelGGL(adamw::norm_kernel, dim3(1), dim3(adamw::kThreads), 0, s, partial, blocks, most, norm);
 }
 
