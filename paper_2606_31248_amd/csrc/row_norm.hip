@@ -158,6 +158,7 @@ __device__ __forceinline__ void load_vector(const float* base, int64_t at, int g
   if (!base) return;
   Piece<false> p;
   p.load<LIE == kLines ? kWhole : LIE>(base, at, gap, n, size);
+  p.keep<LIE>(n);  // what follows is another group's, and may be NaN
   p.get(v);
 }
 

@@ -229,6 +229,31 @@ def test_rows_that_are_not_finite_stay_alone():
     assert bool(torch.isnan(held.view(-1, 32)[~groups]).all()) and bool(torch.isfinite(held.view(-1, 32)[groups]).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [3, 13, 30, 61, 72, 203, 333, 1001, 1500])
+def test_what_is_not_finite_stays_in_its_row_and_group(width, dtype):
+    """NaN and infinities in the first and last channels of a row, and of a group's vectors, which lie next to other
+    rows' and groups' in memory: the others' results are the same bit for bit."""
+    clean, c = Norm(dtype, 3, 7, width), Norm(dtype, 3, 7, width)
+    want = clean.forward()
+    want = {**want, **clean.backward(want["sum"])}
+    rows = torch.ones(21, dtype=torch.bool, device="cuda")
+    for at, v in ((3, "nan"), (5, "inf")):
+        for t in (c.res, c.x, c.dy, c.dsum):
+            t[at, 0] = t[at, -1] = float(v)
+        rows[at] = False
+    for t in (c.gate, c.scale, c.shift):
+        t[1, 0], t[1, -1] = float("nan"), float("inf")
+    rows[7:14] = False                                       # the rows of group 1
+    out = c.forward()
+    out = {**out, **c.backward(out["sum"])}
+    for n in ("sum", "y", "dres", "dx"):
+        assert torch.equal(out[n][rows], want[n][rows]), n
+    for n in ("dgate", "dscale", "dshift"):
+        assert torch.equal(out[n][2], want[n][2]) and not bool(torch.isfinite(out[n][0, 0])), n
+    c.guards()
+
+
 def test_gradient_by_differences():
     """float32, a loss in 64 bits of the kernel's own forward: central differences of 2^-7 in directions of unit size
     are off by their third order (below 2^-14 of the value here) and by the forward's rounding over 2^-7."""
