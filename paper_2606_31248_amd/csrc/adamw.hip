@@ -1,8 +1,9 @@
 // AdamW over many tensors at once, the 8-bit form of its states, and the norm of all gradients.
 //
 // Every element is read and written once: 28 bytes with states in 32 bits, bf16 gradients
-// and a bf16 copy, 16 with states in 8.  HBM bounds the first (15 operations an element),
-// the second has about 60 operations beside it.  A block takes kParamChunk elements of one
+// and a bf16 copy, 16 with states in 8.  HBM bounds the first (all weights of 24 blocks of
+// 1024 channels: 1520 us, 6.0 TB/s of 6.5 that a copy reaches); the second takes 83 vector
+// instructions an element beside it, two thirds of its time (865 us, 6.1 TB/s).  A block takes kParamChunk elements of one
 // tensor; a lane 4 neighbouring ones at a time, 16 bytes of float32, so that 8 lanes hold a
 // group of the 8-bit states.
 #include "state8.h"
@@ -24,7 +25,8 @@ __device__ __forceinline__ Global<T> global(P* p) {
   return (Global<T>)reinterpret_cast<uintptr_t>(p);
 }
 
-// 16, 8 or 4 bytes that are touched once a step, past the caches' replacement.
+// 16, 8 or 4 bytes that are touched once a step, past the caches' replacement (those weights 1547 us, through the
+// caches 1707; 300 tensors of 5.4 million weights 18.3 and 18.5).
 template <typename T>
 __device__ __forceinline__ T load(Global<const T> p) {
   return __builtin_nontemporal_load(p);
@@ -260,7 +262,8 @@ __device__ __forceinline__ void add_square(double& x, float v) { x = fma((double
 
 // Squares of float32 values in float64: neither range nor digits are lost, whatever the count.
 // A block takes kRun neighbouring chunks at a time: where they are of one tensor, all of a
-// lane's loads, 16 bytes each, are in flight together.
+// lane's loads, 16 bytes each, are in flight together (the bf16 gradients of 24 blocks of
+// 1024 channels: 101 us, with 8 chunks 105, with one 157).
 constexpr int kRun = 4;
 template <bool BF16>
 __device__ __forceinline__ void square_run(const ParamRecord& t, int64_t base, double& x, double& y) {
@@ -321,6 +324,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double* partial, i
   if (threadIdx.x == 0) store_norm(x, most, norm);
 }
 
+// Those gradients with 512, 1024, 2048, 4096 blocks, at two places in memory: 156 and 169 us, 99 and 120, 102 and 114,
+// 104 and 113.
 constexpr int kNormBlocks = 2048;
 
 }  // namespace adamw

@@ -349,6 +349,37 @@ def test_beyond_32_bit_offsets():
     torch.cuda.empty_cache()
 
 
+def test_the_most_places_of_8_bits():
+    """2^32 - 64 places: groups at both ends and around 2^31 against the oracle, all others stay zeros."""
+    n = (1 << 32) - 64
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    w = B.make_params([p], [g])
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(n // 32, dtype=torch.uint8, device="cuda") for _ in range(2))
+    places = [0, 32, (1 << 31) - 32, 1 << 31, n - 32]
+    for i, at in enumerate(places):
+        g[at:at + 32] = (1e-3 * torch.randn(32, generator=gen(i))).bfloat16().cuda()
+    B.strata_adamw(B.make_adamw_desc(1e-3, 1, seed=77), w, m, v, ms, vs)
+    for at in places:
+        m32, v32 = T.moments32(f64(g[at:at + 32]), np.zeros(32), np.zeros(32), 0.9, 0.999)
+        r = T.random_numbers(77, np.arange(at, at + 32))
+        for codes, scales, x, random, second in ((m, ms, m32, r[0], False), (v, vs, v32, r[1], True)):
+            want, e = T.encode(x, random, second)
+            assert np.array_equal(codes[at:at + 32].cpu().numpy(), want) and int(scales[at // 32]) == e[0]
+            codes[at:at + 32] = 0
+        d = f64(g[at:at + 32])
+        step = 1e-3 * d / (np.abs(d) + 1e-8)                    # the first: m / (1 - beta1) = g, v / (1 - beta2) = g^2
+        assert np.all(np.abs(f64(p[at:at + 32]) + step) <= UPDATE * np.abs(step))
+        p[at:at + 32] = 0.0
+    for t in (m, v, p):
+        for part in t.split(1 << 30):
+            assert not bool(part.any())
+    for scales, second in ((ms, False), (vs, True)):
+        assert int((scales != T.UNIT[second] + 1).sum()) == len(places)       # groups of zeros have the least scale
+    del p, g, w, m, v, ms, vs, part, t
+    torch.cuda.empty_cache()
+
+
 def test_refusals():
     w = Weights([64, 33], "f32")
     p, g, c = w.p, w.g, w.copies

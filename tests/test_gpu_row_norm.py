@@ -337,6 +337,47 @@ def test_beyond_32_bit_offsets():
     torch.cuda.empty_cache()
 
 
+def test_the_most_rows():
+    """2^31 - 1 rows of 3 channels: the last ones against the oracle, all others alike."""
+    width, rows = 3, (1 << 31) - 1
+    res, y = (torch.empty((rows, width), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    res.fill_(2.0)
+    places = [0, 1, (1 << 30), rows - 3, rows - 2, rows - 1]
+    for i, at in enumerate(places):
+        res[at] = normal((width,), "bf16", gen(i))
+    scale = torch.tensor([[1.0, -0.5, 3.0]], device="cuda")
+    d = B.make_norm_desc(res, eps=EPS)
+    B.strata_residual_norm(d, None, None, res, scale, None, None, y)
+    want, _, _ = T.norm(f64(res[places])[None], f64(scale), eps=EPS)
+    within(f64(y[places]), want[0], HALF_STEP["bf16"] * np.abs(want[0]) * (1 + ARITH) + 2 * ARITH * np.abs(want[0]), "y")
+    one = y[2].clone()
+    y[places] = one
+    for part in y.split(1 << 28):
+        assert bool((part == one).all())
+    del part
+    dy = y.fill_(0.0)
+    for i, at in enumerate(places):
+        dy[at] = normal((width,), "bf16", gen(40 + i))
+    up = f64(dy[places])
+    dscale, ws = torch.empty_like(scale), torch.empty(B.strata_residual_norm_bwd_workspace_size(d), dtype=torch.uint8, device="cuda")
+    B.strata_residual_norm_bwd(d, res, None, None, scale, dy, None, dy, dscale=dscale, workspace=ws)
+    want = T.norm_backward(f64(res[places])[None], up[None], scale=f64(scale), eps=EPS)
+    within(f64(dy[places]), want["dres"][0], HALF_STEP["bf16"] * np.abs(want["dres"][0]) + 2 * ROW_GRAD * want["mag_dres"][0], "dres")
+    within(f64(dscale), want["dscale"], VECTOR_GRAD * want["mag_dscale"], "dscale")
+    dy[places] = 0.0
+    for part in dy.split(1 << 28):
+        assert not bool(part.any())
+    del res, y, dy, part
+    torch.cuda.empty_cache()
+
+
+def test_more_groups_than_a_row_of_blocks():
+    """2^20 + 5 groups of one row: blocks beyond one dimension of the grid, vectors' gradients final at once."""
+    groups, width = (1 << 20) + 5, 8
+    c = Norm("f32", groups, 1, width)
+    check(c)
+
+
 def test_refusals():
     c = Norm("bf16", 2, 4, 64, "x gate scale shift dsum codes")
     o = c.forward()
