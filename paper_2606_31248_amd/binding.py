@@ -77,6 +77,19 @@ class NormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("group_rows", ctypes.c_int64), ("width", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_sizes", None)
+        super().__setattr__(name, value)
+
+    def sizes(self):
+        """(rows, width, elements, groups, dtype), kept until a field is assigned: reading them from C takes 1 us."""
+        known = self.__dict__.get("_sizes")
+        if known is None:
+            rows, per, width = self.rows, self.group_rows, self.width
+            known = self.__dict__["_sizes"] = (rows, width, rows * width, rows // per if per > 0 else 0,
+                                               _torch_dtype(self.dtype))
+        return known
+
 
 class ParamEntry(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
@@ -665,65 +678,77 @@ def make_norm_desc(rows, group_rows: Optional[int] = None, eps: float = 1e-6) ->
     return NormDesc(many, many if group_rows is None else group_rows, width, float(eps), _dtype(rows))
 
 
-def _rows_at(name, t, n, width, dt, index):
-    """The address of a tensor of n elements in rows of `width`, of dtype `dt` on GPU `index`; None for None."""
+_Tensor, _float32 = torch.Tensor, torch.float32
+
+
+def _rows_at(name, t, like, size, dt, index):
+    """The address of a tensor of dtype `dt` on GPU `index` that has the shape `like`, or another of as many rows of
+    the same width (size: rows, width, elements, ...); None for None."""
     if t is None:
         return None
-    if not (type(t) is torch.Tensor and t.dtype is dt and t.get_device() == index and t.is_contiguous() and t.numel() == n
-            and t.shape[-1] == width):
+    if not (t.__class__ is _Tensor and t.dtype is dt and t.get_device() == index and t.is_contiguous()
+            and (t.shape == like or t.numel() == size[2] and t.shape[-1] == size[1])):
         _need(name, t, None, dt, torch.device("cuda", index))
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {n // max(width, 1)} rows of {width}")
+        if t.numel() != size[2] or not t.ndim or t.shape[-1] != size[1]:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {size[0]} rows of {size[1]}")
     return t.data_ptr()
 
 
-def _vector_at(name, t, groups, width, index):
-    """The same for float32 [groups, width] ([width] for a single group)."""
+def _vector_at(name, t, shape, index):
+    """The same for float32 of exactly this shape, [groups, width], or [width] for a single group."""
     if t is None:
         return None
-    if not (type(t) is torch.Tensor and t.dtype is torch.float32 and t.get_device() == index and t.is_contiguous()
-            and (t.shape == (groups, width) or groups == 1 and t.shape == (width,))):
-        _need(name, t, (groups, width), torch.float32, torch.device("cuda", index))
+    if not (t.__class__ is _Tensor and t.dtype is _float32 and t.get_device() == index and t.is_contiguous()
+            and (t.shape == shape or shape[0] == 1 and t.shape == shape[1:])):
+        _need(name, t, shape, torch.float32, torch.device("cuda", index))
     return t.data_ptr()
 
 
 def _norm_common(desc: NormDesc, name, t):
-    """(elements, rows' width, groups, dtype, GPU of `t`)"""
-    dt, width, rows, per = _torch_dtype(desc.dtype), desc.width, desc.rows, desc.group_rows
-    if not (type(t) is torch.Tensor and t.is_cuda):
-        _need(name, t, None, dt)
-    return rows * width, width, rows // per if per > 0 else 0, dt, t.get_device()
+    """(sizes, shape of a vector, dtype, shape of `t`, its GPU)"""
+    size = desc.sizes()
+    if not (t.__class__ is _Tensor and t.is_cuda):
+        _need(name, t, None, size[4])
+    return size, (size[3], size[1]), size[4], t.shape, t.get_device()
 
 
 def strata_residual_norm(desc: NormDesc, x, gate, res, scale, shift, sum, y=None, codes=None, scales=None, stream=None):
     """sum = res + gate x, y = its RMS norm with scale and shift, and / or y in 8 bits (codes int8 of y's shape,
     scales uint8 of a 32nd of its elements).  Without x (gate and sum None) the norm of res."""
-    n, w, groups, dt, i = _norm_common(desc, "res", res)
+    size, vec, dt, like, i = _norm_common(desc, "res", res)
     if scales is not None:
         _need("scales", scales, None, torch.uint8, res.device)
-        if scales.numel() != n // 32:
-            raise ValueError(f"scales: {scales.numel()} elements, expected {n // 32}")
-    _check(load().strata_residual_norm(
-        ctypes.byref(desc), _rows_at("x", x, n, w, dt, i), _vector_at("gate", gate, groups, w, i),
-        _rows_at("res", res, n, w, dt, i), _vector_at("scale", scale, groups, w, i), _vector_at("shift", shift, groups, w, i),
-        _rows_at("sum", sum, n, w, dt, i), _rows_at("y", y, n, w, dt, i), _rows_at("codes", codes, n, w, torch.int8, i),
-        None if scales is None else scales.data_ptr(), _on_gpu(i, stream)))
+        if scales.numel() != size[2] // 32:
+            raise ValueError(f"scales: {scales.numel()} elements, expected {size[2] // 32}")
+        scales = scales.data_ptr()
+        codes = _rows_at("codes", codes, like, size, torch.int8, i)
+    elif codes is not None:
+        codes = _rows_at("codes", codes, like, size, torch.int8, i)
+    st = (_lib or load()).strata_residual_norm(
+        ctypes.byref(desc), _rows_at("x", x, like, size, dt, i), _vector_at("gate", gate, vec, i),
+        _rows_at("res", res, like, size, dt, i), _vector_at("scale", scale, vec, i), _vector_at("shift", shift, vec, i),
+        _rows_at("sum", sum, like, size, dt, i), _rows_at("y", y, like, size, dt, i), codes, scales, _on_gpu(i, stream))
+    if st:
+        _check(st)
 
 
 def strata_residual_norm_bwd_workspace_size(desc: NormDesc) -> int:
-    return int(load().strata_residual_norm_bwd_workspace_size(ctypes.byref(desc)))
+    return (_lib or load()).strata_residual_norm_bwd_workspace_size(ctypes.byref(desc))
 
 
 def strata_residual_norm_bwd(desc: NormDesc, sum, x, gate, scale, dy, dsum, dres, dx=None, dgate=None, dscale=None,
                              dshift=None, workspace=None, stream=None):
     """Gradients dres (and dx, with a gate) of the rows and dgate, dscale, dshift of the vectors for dy and dsum."""
-    n, w, groups, dt, i = _norm_common(desc, "sum", sum)
+    size, vec, dt, like, i = _norm_common(desc, "sum", sum)
     at, nbytes = _workspace_at(workspace, i)
-    _check(load().strata_residual_norm_bwd(
-        ctypes.byref(desc), _rows_at("sum", sum, n, w, dt, i), _rows_at("x", x, n, w, dt, i),
-        _vector_at("gate", gate, groups, w, i), _vector_at("scale", scale, groups, w, i), _rows_at("dy", dy, n, w, dt, i),
-        _rows_at("dsum", dsum, n, w, dt, i), _rows_at("dres", dres, n, w, dt, i), _rows_at("dx", dx, n, w, dt, i),
-        _vector_at("dgate", dgate, groups, w, i), _vector_at("dscale", dscale, groups, w, i),
-        _vector_at("dshift", dshift, groups, w, i), at, nbytes, _on_gpu(i, stream)))
+    st = (_lib or load()).strata_residual_norm_bwd(
+        ctypes.byref(desc), _rows_at("sum", sum, like, size, dt, i), _rows_at("x", x, like, size, dt, i),
+        _vector_at("gate", gate, vec, i), _vector_at("scale", scale, vec, i), _rows_at("dy", dy, like, size, dt, i),
+        _rows_at("dsum", dsum, like, size, dt, i), _rows_at("dres", dres, like, size, dt, i),
+        _rows_at("dx", dx, like, size, dt, i), _vector_at("dgate", dgate, vec, i), _vector_at("dscale", dscale, vec, i),
+        _vector_at("dshift", dshift, vec, i), at, nbytes, _on_gpu(i, stream))
+    if st:
+        _check(st)
 
 
 class Params:
@@ -772,14 +797,16 @@ def make_params(p, g, copies=None) -> Params:
 
 
 def strata_grad_norm_workspace_size(params: Params) -> int:
-    return int(load().strata_grad_norm_workspace_size(ctypes.byref(params.desc)))
+    return (_lib or load()).strata_grad_norm_workspace_size(ctypes.byref(params.desc))
 
 
 def strata_grad_norm(params: Params, max_norm, norm, workspace, stream=None):
     """norm (float32 [2]): the norm of all gradients and the factor that brings it to max_norm at most."""
     i = params.index
-    at, (ws, nbytes) = _vector_at("norm", norm, 1, 2, i), _workspace_at(workspace, i)
-    _check(load().strata_grad_norm(ctypes.byref(params.desc), max_norm, at, ws, nbytes, _on_gpu(i, stream)))
+    at, (ws, nbytes) = _flat_at("norm", norm, 2, _float32, i), _workspace_at(workspace, i)
+    st = (_lib or load()).strata_grad_norm(ctypes.byref(params.desc), max_norm, at, ws, nbytes, _on_gpu(i, stream))
+    if st:
+        _check(st)
 
 
 def make_adamw_desc(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0) -> AdamWDesc:
@@ -789,7 +816,7 @@ def make_adamw_desc(lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0
 
 def _flat_at(name, t, n, dt, index):
     """The address of a tensor [n] of dtype `dt` on GPU `index`."""
-    if not (type(t) is torch.Tensor and t.dtype is dt and t.get_device() == index and t.shape == (n,) and t.is_contiguous()):
+    if not (t.__class__ is _Tensor and t.dtype is dt and t.get_device() == index and t.shape == (n,) and t.is_contiguous()):
         _need(name, t, (n,), dt, torch.device("cuda", index))
     return t.data_ptr() or None
 
@@ -804,8 +831,10 @@ def strata_adamw(desc: AdamWDesc, params: Params, m, v, m_scales=None, v_scales=
         u8 = torch.uint8
         at = (_flat_at("m", m, n, u8, i), _flat_at("v", v, n, u8, i), _flat_at("m_scales", m_scales, n // 32, u8, i),
               _flat_at("v_scales", v_scales, n // 32, u8, i))
-    f = None if factor is None else _flat_at("factor", factor, 1, torch.float32, i)
-    _check(load().strata_adamw(ctypes.byref(desc), ctypes.byref(params.desc), *at, f, _on_gpu(i, stream)))
+    f = None if factor is None else _flat_at("factor", factor, 1, _float32, i)
+    st = (_lib or load()).strata_adamw(ctypes.byref(desc), ctypes.byref(params.desc), *at, f, _on_gpu(i, stream))
+    if st:
+        _check(st)
 
 
 def strata_adamw_unpack(codes, scales, values, second, stream=None):

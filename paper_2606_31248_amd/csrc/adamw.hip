@@ -286,7 +286,8 @@ __device__ __forceinline__ void square_run(const ParamRecord& t, int64_t base, d
 
 __global__ void __launch_bounds__(kThreads) squares_kernel(const ParamRecord* tensors, const int32_t* owner,
                                                            int64_t chunks, double* partial, double most, float* norm) {
-  constexpr int kParts = kParamChunk / kSpan, kAll = kRun * kParamChunk;
+  static_assert(kRun * 64 == kThreads, "a wave for each chunk of a run");
+  constexpr int kAll = kRun * kParamChunk;
   double x = 0., y = 0.;
   for (int64_t run = (int64_t)blockIdx.x * kRun; run < chunks; run += (int64_t)gridDim.x * kRun) {
     const int64_t last = run + kRun <= chunks ? run + kRun - 1 : chunks - 1;
@@ -296,17 +297,21 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const ParamRecord* te
       t.bf16 ? square_run<true>(t, base, x, y) : square_run<false>(t, base, x, y);
       continue;
     }
-    for (int64_t chunk = run; chunk <= last; ++chunk) {
-      const ParamRecord u = tensors[owner[chunk]];
-      const int64_t first = (chunk - u.chunk) * kParamChunk + 4 * threadIdx.x;
+    // a wave each, with all loads in flight
+    const int64_t chunk = run + (threadIdx.x >> 6);
+    if (chunk > last) continue;
+    const ParamRecord u = tensors[owner[chunk]];
+    const int64_t first = (chunk - u.chunk) * kParamChunk + 4 * (threadIdx.x & 63);
+    float g[kParamChunk / 256][4];
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) {
-        const int64_t at = first + i * kSpan, left = u.n - at;
-        float g[4];
-        load_grads(u, at, left >= 4 ? 4 : left > 0 ? (int)left : 0, g);
+    for (int i = 0; i < kParamChunk / 256; ++i) {
+      const int64_t at = first + i * 256, left = u.n - at;
+      load_grads(u, at, left >= 4 ? 4 : left > 0 ? (int)left : 0, g[i]);
+    }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) add_square(j & 1 ? y : x, g[j]);
-      }
+    for (int i = 0; i < kParamChunk / 256; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add_square(j & 1 ? y : x, g[i][j]);
     }
   }
   x = block_sum(x + y);
@@ -359,7 +364,7 @@ void launch_adamw_unpack(const uint8_t* codes, const uint8_t* scales, int64_t n,
 
 int64_t grad_norm_blocks(int64_t chunks) {
   const int64_t runs = (chunks + adamw::kRun - 1) / adamw::kRun;
-  return runs <= 2 ? chunks > 0 : runs < adamw::kNormBlocks ? runs : adamw::kNormBlocks;  // one block: one launch
+  return runs <= 4 ? chunks > 0 : runs < adamw::kNormBlocks ? runs : adamw::kNormBlocks;  // one block: one launch
 }
 
 void launch_grad_norm(const ParamRecord* tensors, const int32_t* owner, int64_t chunks, double most, float* norm,

@@ -558,6 +558,7 @@ static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
 static int64_t chunks_of(const NormArgs& a, bool bf16, bool all) {
   const int teams = shape_of(a.width, true).teams;
   const int64_t most = (a.group_rows + teams - 1) / teams;
+  if (most <= 4) return 1;  // a second launch would take longer
   // partial sums of 16 MiB, or a block's for 12 rows, a tenth of what these move in bf16
   const int64_t room = std::max<int64_t>((16 << 20) / (3 * 4 * a.width), a.rows / 12);
   const int64_t fill = std::min(room, bwd_blocks(a, bf16, all));
