@@ -361,7 +361,7 @@ strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int
 typedef struct {
   int64_t rows;       /* 1 to 2^31 - 1, rows * width below 2^40 */
   int64_t group_rows; /* divides rows */
-  int32_t width;      /* 1 to 8192; a multiple of 8 is fastest */
+  int32_t width;      /* 1 to 8192; whole 16 bytes of dtype are fastest */
   float eps;          /* finite, >= 0 */
   strata_dtype dtype; /* x, res, sum, y and the gradients of the rows */
 } strata_norm_desc;

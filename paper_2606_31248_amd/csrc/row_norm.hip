@@ -26,8 +26,8 @@ struct Part {
   int lo, hi;  // of the first and the second 4
 };
 
-// How a row lies: kLines, whole cache lines that are streamed; kWhole, a multiple of 8
-// channels, so that 4 are there or none; kRagged, of any width.
+// How a row lies: kLines, whole cache lines that are streamed; kWhole, whole 16 bytes, so
+// that a lane's 8 channels, of float32 each 4 of them, are there or not; kRagged, of any width.
 enum Lie { kLines, kWhole, kRagged };
 
 // Four elements, 16 bytes of float32, from any address of the type's alignment.  Of a ragged
@@ -149,8 +149,9 @@ struct Piece<false> {
   }
 };
 
-// A lane's part of a vector, float32 and read again by other rows.
-template <int LIE>
+// A lane's part of a vector, float32 and read again by other rows.  KEEP: 0 behind a ragged
+// row's end, where another group's vector begins, which may be NaN.
+template <int LIE, bool KEEP = false>
 __device__ __forceinline__ void load_vector(const float* base, int64_t at, int gap, Part n, int64_t size, float fill,
                                             float (&v)[8]) {
 #pragma unroll
@@ -158,7 +159,7 @@ __device__ __forceinline__ void load_vector(const float* base, int64_t at, int g
   if (!base) return;
   Piece<false> p;
   p.load<LIE == kLines ? kWhole : LIE>(base, at, gap, n, size);
-  p.keep<LIE>(n);  // what follows is another group's, and may be NaN
+  if (KEEP) p.keep<LIE>(n);
   p.get(v);
 }
 
@@ -253,8 +254,8 @@ __device__ __forceinline__ uint32_t over_eight(uint32_t t) {
 // A team takes one row, so that what is in flight is a narrow band of each tensor's rows, and
 // finds the vectors in the caches.  Training tile (2^18 rows of 1024, bf16): 6.3 TB/s; 6.0
 // with 256 blocks that keep the vectors in registers and load a row ahead, 5.4 with 1024.
-// Ragged rows, whose vectors take many instructions to load: where there are more blocks than
-// fit the card a team takes several, loading a row ahead (rows of 33: 4.1 against 3.4 TB/s).
+// Ragged rows of bf16 whose vectors take many instructions to load: where there are more blocks
+// than fit the card a team takes several, loading a row ahead.
 template <bool BF16, int LANES, int PIECES, bool BLOCK, int LIE>
 __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) fwd_kernel(const NormArgs a) {
   __shared__ float sums[2][kMaxWaves];
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) fwd_kern
   Part n[PIECES];
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) n[i] = at.part(i, width);
-  constexpr bool kSeveral = LIE == kRagged;
+  constexpr bool kSeveral = BF16 && LIE == kRagged;
   const int64_t size = a.rows * width, stride = a.blocks * at.teams;
   Piece<BF16> s[PIECES], x[PIECES], next_s[PIECES], next_x[PIECES];
   auto fetch = [&](int64_t t) {
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(BLOCK ? kMaxWaves * 64 : kWaves * 64) bwd_kern
   for (int i = 0; i < PIECES; ++i) {
     const int64_t c = b * width + at.first + i * at.step;
     if (ALL) load_vector<LIE>(a.gate, c, at.gap, n[i], a.groups * width, 1.f, gate[i]);
-    load_vector<LIE>(a.scale, c, at.gap, n[i], a.groups * width, 1.f, scale[i]);
+    load_vector<LIE, true>(a.scale, c, at.gap, n[i], a.groups * width, 1.f, scale[i]);
   }
   const int64_t last = (b + 1) * a.group_rows, stride = a.chunks * at.teams;
   int64_t t = b * a.group_rows + chunk * at.teams + at.team;
@@ -531,11 +532,15 @@ static Shape shape_of(int width, bool back) {
   return {lanes, lanes * 8 < width ? 2 : 1, kWaves * 64, kWaves * 64 / lanes};
 }
 
-// Blocks of the forward: a row for each team, but short ragged rows.
-static int64_t fwd_blocks(const NormArgs& a) {
+static bool ragged(const NormArgs& a, bool bf16) { return a.width % (bf16 ? 8 : 4); }
+
+// Blocks of the forward: a row for each team, but in ragged rows of bf16 that are short or have a gate or a shift (TB/s
+// with 1024 blocks and with all: rows of 33 4.1, 3.4; with a gate, of 203 4.5, 4.1, of 1293 3.4, 3.0; of 203 without one
+// 4.6, 4.7; in float32 of 33 4.6, 5.0, of 203 4.8, 5.6).
+static int64_t fwd_blocks(const NormArgs& a, bool bf16) {
   const int teams = shape_of(a.width, false).teams;
   const int64_t all = (a.rows + teams - 1) / teams;
-  return a.width % 8 && a.width <= 512 && all > 1024 ? 1024 : all;
+  return bf16 && ragged(a, bf16) && (a.width <= 64 || a.gate || a.shift) ? std::min<int64_t>(all, 1024) : all;
 }
 
 // Blocks of the backward, which write a row of partial sums each: few waves with much in flight each read faster than
@@ -551,7 +556,7 @@ static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
     const int waves = at.threads / 64, want = all ? 4 : 8;
     return waves >= want ? kCus : kCus * (want / waves);
   }
-  const int want = a.width % 8 ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1;
+  const int want = ragged(a, bf16) ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1;
   return a.rows >= (int64_t)kCus * want * 8 * at.teams ? kCus * want : kCus;
 }
 
@@ -613,7 +618,7 @@ static void run(const NormArgs& a, bool back, hipStream_t s) {
 
 template <bool BF16>
 static void run(const NormArgs& a, bool back, hipStream_t s) {
-  if (a.width % 8) return run<BF16, kRagged>(a, back, s);
+  if (ragged(a, BF16)) return run<BF16, kRagged>(a, back, s);
   streams(a, BF16) ? run<BF16, kLines>(a, back, s) : run<BF16, kWhole>(a, back, s);
 }
 
@@ -621,7 +626,7 @@ static void run(const NormArgs& a, bool back, hipStream_t s) {
 
 void launch_residual_norm(NormArgs a, strata_dtype dt, hipStream_t s) {
   a.by_group = fast_div(a.group_rows);
-  a.blocks = row_norm::fwd_blocks(a);
+  a.blocks = row_norm::fwd_blocks(a, dt == STRATA_BF16);
   dt == STRATA_BF16 ? row_norm::run<true>(a, false, s) : row_norm::run<false>(a, false, s);
 }
 

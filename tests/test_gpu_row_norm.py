@@ -123,8 +123,8 @@ def check(c, shift=True):
 
 
 # widths on both sides of every team of lanes, of one and two pieces a lane, of a wave and of 2 to 8 waves
-WIDTHS = [1, 2, 7, 8, 9, 31, 32, 33, 40, 63, 64, 65, 127, 128, 129, 203, 256, 257, 509, 512, 513, 520, 768, 1000, 1023, 1024,
-          1025, 1032, 1536, 2047, 2048, 2049, 4096, 5000, 8185, 8191, 8192]
+WIDTHS = [1, 2, 4, 7, 8, 9, 12, 31, 32, 33, 40, 63, 64, 65, 127, 128, 129, 132, 203, 204, 256, 257, 509, 512, 513, 520, 768, 1000, 1023, 1024,
+          1025, 1028, 1032, 1132, 1536, 2047, 2048, 2049, 4096, 5000, 8185, 8191, 8192]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
