@@ -354,8 +354,8 @@ strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int
  * (strata_ckpt_pack's of y, bit for bit: codes int8 [rows, width], scales uint8
  * [rows, width / 32], for a width of whole 32), or both; what is not wanted is NULL.
  * Arithmetic and sums in float32.  Range of the norm, here and in the backward: a row of
- * root mean square 2^64 / sqrt(width) and more has squares that overflow, and a norm and
- * a gradient of 0; with eps below 2^-126 a mean square below 2^-126 keeps fewer digits
+ * root mean square 2^64 / sqrt(width) and more has squares that overflow, a norm of 0 and
+ * no gradient through it; with eps below 2^-126 a mean square below 2^-126 keeps fewer digits
  * and one of 0 makes the row NaN.
  * sum may be res or x itself; no other buffers may overlap. */
 typedef struct {
