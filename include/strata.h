@@ -437,8 +437,9 @@ strata_status strata_grad_norm(const strata_params* params, double max_norm, flo
  * group's scale: a code c of m has a sign (bit 7) and magnitude k = c mod 128, one of v the
  * magnitude k = c, and stands for f(k) 2^(max(E - U, 1) - 127), U = 17 (m) or 33 (v), f(k) =
  * k below 8 and (8 + k mod 8) 2^(k div 8 - 1) above: 3 bits behind the leading one down to 8
- * units.  E is the biased exponent of the group's largest value after the step (one more
- * from 1.875 times the power of two on), at least U + 1.  A value is rounded to one of its
+ * units.  E is the biased exponent of the group's largest value after the step (one
+ * more from 1.875 times the power of two on), at least U + 1 and at most 254, where the
+ * largest code stands for all above it.  A value is rounded to one of its
  * two neighbours, up with the probability of its distance to the lower, so that a state
  * moves by less than a code's step (beta2 = 0.999 moves v by a thousandth) in the mean as it
  * should; v above 0 keeps at least code 1.  The random numbers are a hash of (seed, place):

@@ -76,6 +76,7 @@ def encode(x, random, second):
     # in steps: the sum below 8 is rounded as float32 rounds it, above it is exact
     part = np.floor((np.ldexp(t, 3 - octave).astype(np.float32) + np.asarray(random, np.float32).reshape(-1, 32)))
     code = (octave - 3) * 8 + part.astype(np.int64)
+    code = np.minimum(code, 255 if second else 127)                    # at the largest exponent
     if second:
         code = np.where(a > 0, np.maximum(code, 1), code)
     else:

@@ -52,15 +52,16 @@ __device__ __forceinline__ float decode(uint32_t byte, float unit) {
 
 // Rounded up where `random`, 16 bits, reaches over the border: the mean over the random
 // numbers is x.  A second moment above 0 keeps code 1: it is divided by.  Without branches:
-// the code of the part below 8 and that of the part above, one of which is 8.
+// the code of the part below 8 and that of the part above, one of which is 8.  Only at the
+// largest scale, which cannot be one more, is there a code too many.
 template <bool SECOND>
 __device__ __forceinline__ uint32_t encode(float x, float per_unit, uint32_t random) {
   const float t = fabsf(x) * per_unit;
   const uint32_t low = (uint32_t)(fminf(t, 8.f) + (float)random * 0x1p-16f);
   const uint32_t high = (__float_as_uint(fmaxf(t, 8.f)) + (random << 4)) >> 20;
   const uint32_t c = low + high - (kBits + 8u);
-  if (SECOND) return umax(c, x > 0.f ? 1u : 0u);
-  return c | (__float_as_uint(x) >> 24 & 128u);
+  if (SECOND) return min(umax(c, x > 0.f ? 1u : 0u), 255u);
+  return min(c, 127u) | (__float_as_uint(x) >> 24 & 128u);
 }
 
 // 32 bits of (seed, element): two rounds of a product and a shift, which move every bit.

@@ -150,6 +150,25 @@ def test_sizes_of_gradients(size, eight):
     Weights([2000, 70], "f32", eight=eight, seed=3, grad_size=size).check_step(eps=2.0 ** -100)
 
 
+def test_states_at_the_end_of_the_range():
+    """Values from 1.875 times 2^127 on have no larger scale: the largest code, and no other value's bits touched."""
+    w = Weights([64, 64], "f32", eight=True, seed=4)
+    w.g[0].mul_(1e-3)
+    w.g[0][:32] = torch.linspace(-3.4e38, 3.4e38, 32, dtype=torch.float64).float()   # m; its range overflows in float32
+    w.g[1][::2] = 1.83e19                                    # its square 3.35e38: v
+    g, was = w.flat(w.g), f64(w.p[0])
+    w.step(beta1=0.0, beta2=0.0, weight_decay=0.0)
+    m32, v32 = T.moments32(g, g * 0, g * 0, 0.0, 0.0)
+    r = T.random_numbers(5, np.arange(128))
+    for codes, scales, x, random, second in ((w.m, w.m_scales, m32, r[0], False), (w.v, w.v_scales, v32, r[1], True)):
+        want, e = T.encode(x, random, second)
+        assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), e)
+    m, v = w.states()
+    assert m[0] == -1.875 * 2.0 ** 127 and m[31] == 1.875 * 2.0 ** 127 and v[64] == 1.875 * 2.0 ** 127
+    assert np.isnan(v[:32]).all() and np.isfinite(v[32:]).all() and np.isfinite(m).all()
+    assert np.array_equal(f64(w.p[0])[:16], was[:16])        # squares beyond float32: a step of m / infinity
+
+
 @pytest.mark.parametrize("eight", [False, True])
 def test_weights_of_zero_gradient(eight):
     """Zero gradients and zero states move nothing but by the decay."""
