@@ -521,24 +521,29 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const NormArgs a) {
 struct Shape {
   int lanes, pieces, threads, teams;
 };
-static Shape shape_of(int width, bool back) {
+static bool ragged(const NormArgs& a, bool bf16) { return a.width % (bf16 ? 8 : 4); }
+// Ragged rows, of a wave's piece at most, that are too few to fill the card with a wave a SIMD.
+static bool few(const NormArgs& a, bool bf16) { return ragged(a, bf16) && a.width <= 512 && a.rows < 1 << 16; }
+
+static Shape shape_of(const NormArgs& a, bool bf16, bool back) {
   constexpr int kWave = 64 * 8;  // channels of a wave's piece
+  const int width = a.width;
   if (width > 2 * kWave) return {64, 2, 64 * ((width + 2 * kWave - 1) / (2 * kWave)), 1};
   // Two pieces a lane in the backward where rows are long enough for 8 lanes: half as many exchanges an element, and a
-  // wave has twice as much in flight.  The forward has more waves in flight instead (rows of 512: 6.5 and 6.2 TB/s).
-  const int most = width > 64 && back ? 2 : 1;
+  // wave has twice as much in flight.  The forward has more waves in flight instead (rows of 512: 6.5 and 6.2 TB/s), and
+  // so do few ragged rows (15876 of 203 in float32 21.2 us with two pieces and 256 blocks, 18.9 with one and 512; of 999,
+  // which take two anyway, 42.6 and 43.6).
+  const int most = width > 64 && back && !few(a, bf16) ? 2 : 1;
   int lanes = width % 32 ? 1 : 8;  // 8 lanes hold the float32 values of a group of codes
   while (lanes < 64 && lanes * 8 * most < width) lanes *= 2;
   return {lanes, lanes * 8 < width ? 2 : 1, kWaves * 64, kWaves * 64 / lanes};
 }
 
-static bool ragged(const NormArgs& a, bool bf16) { return a.width % (bf16 ? 8 : 4); }
-
 // Blocks of the forward: a row for each team, but in ragged rows of bf16 that are short or have a gate or a shift (TB/s
 // with 1024 blocks and with all: rows of 33 4.1, 3.4; with a gate, of 203 4.5, 4.1, of 1293 3.4, 3.0; of 203 without one
 // 4.6, 4.7; in float32 of 33 4.6, 5.0, of 203 4.8, 5.6).
 static int64_t fwd_blocks(const NormArgs& a, bool bf16) {
-  const int teams = shape_of(a.width, false).teams;
+  const int teams = shape_of(a, bf16, false).teams;
   const int64_t all = (a.rows + teams - 1) / teams;
   return bf16 && ragged(a, bf16) && (a.width <= 64 || a.gate || a.shift) ? std::min<int64_t>(all, 1024) : all;
 }
@@ -547,21 +552,22 @@ static int64_t fwd_blocks(const NormArgs& a, bool bf16) {
 // many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.8, 5.5; with a
 // gate 5.9, 5.0, 5.4), two where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's
 // two more streams and three sums (rows of 4096 5.9, 5.5, 5.3).  If rows are many, ragged ones two (rows of 201: 4.3,
-// 5.0, 4.8; 15876 rows of 203: 3.7, 3.0) or, short ones with a piece a lane, four (rows of 33: 2.4, 3.2, 4.2), and gated ones of float32 four (5.2,
+// 5.0, 4.8) or, short ones with a piece a lane, four (rows of 33: 2.4, 3.2, 4.2), and gated ones of float32 four (5.2,
 // 5.7, 6.0).
 constexpr int kCus = 256;
 static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
-  const Shape at = shape_of(a.width, true);
+  const Shape at = shape_of(a, bf16, true);
   if (at.teams == 1) {
     const int waves = at.threads / 64, want = all ? 4 : 8;
     return waves >= want ? kCus : kCus * (want / waves);
   }
+  if (few(a, bf16)) return 2 * kCus;
   const int want = ragged(a, bf16) ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1;
   return a.rows >= (int64_t)kCus * want * 8 * at.teams ? kCus * want : kCus;
 }
 
 static int64_t chunks_of(const NormArgs& a, bool bf16, bool all) {
-  const int teams = shape_of(a.width, true).teams;
+  const int teams = shape_of(a, bf16, true).teams;
   const int64_t most = (a.group_rows + teams - 1) / teams;
   if (most <= 4) return 1;  // a second launch would take longer
   // partial sums of 16 MiB, or a block's for 12 rows, a tenth of what these move in bf16
@@ -595,7 +601,7 @@ static void start(const NormArgs& a, bool back, const Shape& at, hipStream_t s) 
 
 template <bool BF16, int LIE>
 static void run(const NormArgs& a, bool back, hipStream_t s) {
-  const Shape at = shape_of(a.width, back);
+  const Shape at = shape_of(a, BF16, back);
   if (at.teams == 1) return start<BF16, 64, 2, true, LIE>(a, back, at, s);
   if (at.pieces == 1) {
     switch (at.lanes) {
