@@ -681,16 +681,20 @@ def make_norm_desc(rows, group_rows: Optional[int] = None, eps: float = 1e-6) ->
 _Tensor, _float32 = torch.Tensor, torch.float32
 
 
+def _need_rows(name, t, size):
+    if t.numel() != size[2] or not t.ndim or t.shape[-1] != size[1]:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {size[0]} rows of {size[1]}")
+
+
 def _rows_at(name, t, like, size, dt, index):
-    """The address of a tensor of dtype `dt` on GPU `index` that has the shape `like`, or another of as many rows of
-    the same width (size: rows, width, elements, ...); None for None."""
+    """The address of a tensor of dtype `dt` on GPU `index` that has the shape `like`, which _norm_common compared with
+    the descriptor, or another of as many rows of the same width (size: rows, width, elements, ...); None for None."""
     if t is None:
         return None
     if not (t.__class__ is _Tensor and t.dtype is dt and t.get_device() == index and t.is_contiguous()
             and (t.shape == like or t.numel() == size[2] and t.shape[-1] == size[1])):
         _need(name, t, None, dt, torch.device("cuda", index))
-        if t.numel() != size[2] or not t.ndim or t.shape[-1] != size[1]:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {size[0]} rows of {size[1]}")
+        _need_rows(name, t, size)
     return t.data_ptr()
 
 
@@ -705,11 +709,15 @@ def _vector_at(name, t, shape, index):
 
 
 def _norm_common(desc: NormDesc, name, t):
-    """(sizes, shape of a vector, dtype, shape of `t`, its GPU)"""
+    """(sizes, shape of a vector, dtype, shape of `t`, its GPU); refuses a `t` that is not the descriptor's rows, whose
+    shape the other tensors' are then compared with."""
     size = desc.sizes()
     if not (t.__class__ is _Tensor and t.is_cuda):
         _need(name, t, None, size[4])
-    return size, (size[3], size[1]), size[4], t.shape, t.get_device()
+    like = t.shape
+    if not like or like[-1] != size[1] or t.numel() != size[2]:
+        _need_rows(name, t, size)
+    return size, (size[3], size[1]), size[4], like, t.get_device()
 
 
 def strata_residual_norm(desc: NormDesc, x, gate, res, scale, shift, sum, y=None, codes=None, scales=None, stream=None):

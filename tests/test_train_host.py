@@ -206,6 +206,75 @@ def test_binding_rejects_host_tensors():
     assert B.make_norm_desc(torch.zeros(())).rows == 0 and B.make_norm_desc(torch.zeros(0, 8)).rows == 0
 
 
+class OnGpu(torch.Tensor):
+    """A host tensor that says it lies on GPU 0."""
+    is_cuda = True
+    device = property(lambda self: torch.device("cuda", 0))
+
+    def get_device(self):
+        return 0
+
+    @classmethod
+    def __torch_function__(cls, func, types, args=(), kwargs=None):
+        with torch._C.DisableTorchFunctionSubclass():
+            return func(*args, **(kwargs or {}))
+
+
+def on_gpu(shape, dtype=torch.bfloat16):
+    return torch.Tensor._make_subclass(OnGpu, torch.zeros(shape, dtype=dtype))
+
+
+@pytest.fixture
+def launches(monkeypatch):
+    """The library's norm calls as a list of their names: the binding's checks alone, on tensors that need no GPU."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: made.append(name)
+    monkeypatch.setattr(B, "_lib", Library())
+    monkeypatch.setattr(B, "_Tensor", OnGpu)
+    monkeypatch.setattr(B, "_on_gpu", lambda index, stream: None)
+    return made
+
+
+def norm_calls(d, shape):
+    """Forward and backward of descriptor `d` with all row tensors of `shape`."""
+    rows = lambda dtype=torch.bfloat16: on_gpu(shape, dtype)  # noqa: E731
+    vec = lambda: on_gpu((d.rows // d.group_rows, d.width), torch.float32)  # noqa: E731
+    forward = lambda **kw: B.strata_residual_norm(d, **dict(dict(  # noqa: E731
+        x=rows(), gate=vec(), res=rows(), scale=vec(), shift=vec(), sum=rows(), y=rows()), **kw))
+    backward = lambda **kw: B.strata_residual_norm_bwd(d, **dict(dict(  # noqa: E731
+        sum=rows(), x=rows(), gate=vec(), scale=vec(), dy=rows(), dsum=rows(), dres=rows(), dx=rows(), dgate=vec(), dscale=vec(),
+        dshift=vec()), **kw))
+    return forward, backward
+
+
+@pytest.mark.parametrize("shape", [(2, 64), (99, 64), (101, 64), (0, 64), (7, 8), (100, 32), (50, 128), (200, 32), (64,), (6400,),
+                                   (3, 5, 64), (100, 8, 8), ()])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_rows_of_another_descriptor_are_refused(shape, groups, launches):
+    """All row tensors alike, but not the rows that the descriptor counts: a batch smaller than the one it was made for."""
+    d = B.NormDesc(100, 100 // groups, 64, 1e-6, B.STRATA_BF16)
+    for call, name in zip(norm_calls(d, shape), ("res", "sum")):
+        with pytest.raises(ValueError, match=name):
+            call()
+    codes = dict(y=None, codes=on_gpu(shape, torch.int8), scales=on_gpu((100, 2), torch.uint8))
+    with pytest.raises(ValueError, match="res"):
+        norm_calls(d, shape)[0](**codes)
+    assert not launches
+
+
+def test_rows_of_the_descriptor_in_other_shapes(launches):
+    """As many rows of its width in any shape, one another's or not."""
+    d = B.NormDesc(100, 25, 64, 1e-6, B.STRATA_BF16)
+    for shape, other in (((100, 64), (4, 25, 64)), ((4, 5, 5, 64), (100, 64)), ((1, 100, 64), (1, 100, 64))):
+        forward, backward = norm_calls(d, shape)
+        forward(x=on_gpu(other), codes=on_gpu(other, torch.int8), scales=on_gpu((200,), torch.uint8))
+        backward(dy=on_gpu(other), dx=on_gpu(other))
+    assert launches == ["strata_residual_norm", "strata_residual_norm_bwd"] * 3
+
+
 # ---- the oracle ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("second", [False, True])
