@@ -704,7 +704,8 @@ def _vector_at(name, t, shape, index):
         return None
     if not (t.__class__ is _Tensor and t.dtype is _float32 and t.get_device() == index and t.is_contiguous()
             and (t.shape == shape or shape[0] == 1 and t.shape == shape[1:])):
-        _need(name, t, shape, torch.float32, torch.device("cuda", index))
+        single = shape[0] == 1 and isinstance(t, torch.Tensor) and t.dim() == 1
+        _need(name, t, shape[1:] if single else shape, torch.float32, torch.device("cuda", index))
     return t.data_ptr()
 
 

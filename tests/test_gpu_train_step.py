@@ -192,3 +192,19 @@ def test_a_step_of_other_gradients_and_state_size():
         opts.append(opt)
     size = lambda o: sum(t.nbytes for t in (o.m, o.v, o.m_scales, o.v_scales) if t is not None)  # noqa: E731
     assert size(opts[1]) == size(opts[0]) * 33 // 128
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_scale_of_a_module(dtype):
+    """A learned scale as a module holds it, nn.Parameter [width]: the same as [1, width], its gradient in its shape."""
+    g = gen(11)
+    res, x, dy = (normal((50, 64), dtype, g) for _ in range(3))
+    scale = torch.nn.Parameter((1 + 0.2 * torch.randn(64, generator=g)).cuda())
+    got, want = [], []
+    for out, w in ((got, scale), (want, scale.detach()[None])):
+        y, total, saved = pipeline.norm_forward(res, x, scale=w)
+        dres, _, _, dscale, _ = pipeline.norm_backward(saved, dy)
+        assert dscale.shape == w.shape
+        out += [y, total, dres, dscale.view(-1)]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

@@ -275,6 +275,35 @@ def test_rows_of_the_descriptor_in_other_shapes(launches):
     assert launches == ["strata_residual_norm", "strata_residual_norm_bwd"] * 3
 
 
+class Learned(OnGpu):
+    """Of another class than the binding's quick check knows, as nn.Parameter is."""
+
+
+def test_vectors_of_a_single_group(launches):
+    """[width] or [1, width], tensors and parameters alike; no other shape."""
+    d = B.NormDesc(100, 100, 64, 1e-6, B.STRATA_BF16)
+    forward, backward = norm_calls(d, (100, 64))
+    for kind in (OnGpu, Learned):
+        for shape in ((64,), (1, 64)):
+            v = torch.Tensor._make_subclass(kind, torch.zeros(shape))
+            forward(gate=v, scale=v, shift=v)
+            backward(gate=v, scale=v)
+        for shape in ((63,), (65,), (1, 63), (2, 64), (64, 1), (1, 1, 64), ()):
+            v = torch.Tensor._make_subclass(kind, torch.zeros(shape))
+            for call in (lambda: forward(scale=v), lambda: forward(shift=v), lambda: backward(scale=v), lambda: backward(dshift=v)):
+                with pytest.raises(ValueError, match="shape"):
+                    call()
+        v = torch.Tensor._make_subclass(kind, torch.zeros(64, dtype=torch.bfloat16))
+        with pytest.raises(ValueError, match="dtype|float32"):
+            forward(scale=v)
+    assert len(launches) == 8
+    # of several groups: [groups, width] alone
+    forward, _ = norm_calls(B.NormDesc(100, 50, 64, 1e-6, B.STRATA_BF16), (100, 64))
+    for kind in (OnGpu, Learned):
+        with pytest.raises(ValueError, match="scale"):
+            forward(scale=torch.Tensor._make_subclass(kind, torch.zeros(64)))
+
+
 # ---- the oracle ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("second", [False, True])
