@@ -242,13 +242,13 @@ class AdamW:
     def step(self, lr: float) -> Optional[torch.Tensor]:
         """One step from the gradients that are in place.  With max_norm: float32 [2] on the device, the gradients'
         norm and the factor they were multiplied by, overwritten by the next step."""
-        self.steps += 1
-        norm = None
+        norm, k = None, self.steps + 1
         if self.max_norm is not None:
             norm = self._norm
             B.strata_grad_norm(self.params, self.max_norm, norm, self._ws)
-        desc = B.make_adamw_desc(lr, self.steps, seed=(self.seed << 40) + self.steps, **self.hyper)
+        desc = B.make_adamw_desc(lr, k, seed=(self.seed << 40) + k, **self.hyper)
         B.strata_adamw(desc, self.params, self.m, self.v, self.m_scales, self.v_scales, None if norm is None else norm[1:])
+        self.steps = k   # a step that was refused is none
         return norm
 
     def moments(self, i: int):

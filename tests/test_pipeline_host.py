@@ -1,4 +1,4 @@
-"""What a block's saved state says about its lse and output, without a GPU."""
+"""What a block's saved state says about its lse and output, and what an optimiser counts, without a GPU."""
 import pytest
 import torch
 
@@ -25,3 +25,41 @@ def test_the_forwards_own_state():
     s = saved()
     s.out, s.lse, s.gate = s.out.clone(), s.lse.clone(), None      # moved away and back
     assert not s.again and saved(again=True).again
+
+
+class Host:
+    """The binding's calls on host tensors: lists that are only kept, steps that are recorded and, if told to, refused."""
+
+    def __init__(self, monkeypatch):
+        self.steps, self.refuse = [], False
+        for name in ("make_params", "strata_grad_norm_workspace_size", "strata_grad_norm", "strata_adamw"):
+            monkeypatch.setattr(B, name, getattr(self, name))
+
+    def make_params(self, p, g, copies=None):
+        made = B.Params((list(p), list(g), copies), B.ParamList(0, len(p), len(p), 32 * len(p)),
+                        torch.zeros(1, dtype=torch.uint8), [32 * i for i in range(len(p))], torch.device("cpu"))
+        return made
+
+    def strata_grad_norm_workspace_size(self, params):
+        return 0
+
+    def strata_grad_norm(self, params, max_norm, norm, ws):
+        pass
+
+    def strata_adamw(self, desc, params, *states):
+        if self.refuse:
+            raise B.StrataError(B.STRATA_ERR_INVALID_ARG, "refused")
+        self.steps.append((desc.step, desc.seed, params.tensors[1]))
+
+
+def test_a_refused_step_is_not_counted(monkeypatch):
+    host = Host(monkeypatch)
+    opt = pipeline.AdamW([torch.zeros(4)], [torch.zeros(4)], seed=3, max_norm=1.0)
+    opt.step(1e-3)
+    host.refuse = True
+    with pytest.raises(B.StrataError):
+        opt.step(-1.0)
+    assert opt.steps == 1
+    host.refuse = False
+    opt.step(1e-3)
+    assert opt.steps == 2 and [k for k, _, _ in host.steps] == [1, 2] and host.steps[0][1] != host.steps[1][1]
