@@ -220,16 +220,23 @@ def norm_backward(saved: NormSaved, dy, dsum=None):
     return dres, dres if dx is None else dx, dgate, dscale, dshift
 
 
+def _current_stream(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
 class AdamW:
     """AdamW over a list of weights, with the norm of their gradients clipped and the states in 32 bits or in 8.
 
-    p, g, copies: as binding.make_params takes them; the tensors stay where they are.  m, v and, in 8 bits, m_scales
+    p, g, copies: as binding.make_params takes them; the list keeps the tensors alive and takes them to stay where they
+    are.  Gradients that are allocated anew, as where zero_grad sets them to None, are given to `renew` before the step
+    that takes them: a list of weights' own .grad refuses a step on one that was replaced.  m, v and, in 8 bits, m_scales
     and v_scales are the states, flat, and `steps` the steps taken: what a checkpoint stores.  A step whose gradients
     are not all finite changes no tensor if it clips (max_norm, which may be infinity), but is counted."""
 
     def __init__(self, p, g, copies=None, eight_bit: bool = False, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, weight_decay: float = 0.0, max_norm: Optional[float] = None, seed: int = 0):
-        self.params = B.make_params(p, g, copies)
+        self._captured = []
+        self._take(p, g, copies)
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
         self.max_norm, self.seed, self.steps = max_norm, seed, 0
         n, dev = self.params.places, self.params.device
@@ -237,11 +244,26 @@ class AdamW:
         self.m_scales, self.v_scales = ((torch.zeros(n // 32, dtype=torch.uint8, device=dev) for _ in range(2)) if eight_bit
                                         else (None, None))
         self._norm = torch.empty(2, dtype=torch.float32, device=dev)
-        self._ws = torch.empty(B.strata_grad_norm_workspace_size(self.params), dtype=torch.uint8, device=dev)
+
+    def _take(self, p, g, copies):
+        params = B.make_params(p, g, copies)
+        ws = torch.empty(B.strata_grad_norm_workspace_size(params), dtype=torch.uint8, device=params.device)
+        self.params, self._ws, self._stream = params, ws, _current_stream(params.device)
+        self._own = [(w, d) for w, d in zip(*params.tensors[:2]) if d is not None and w.is_leaf and w.grad is d]
+
+    def renew(self, g, copies=None):
+        """Other gradients (None: that tensor is left as it is) and copies (default: the present ones) from the next step
+        on; weights, states and steps stay.  Makes the list's table and copies it to the device, 0.4 ms for 300 tensors:
+        gradients that stay where they are (zero_grad(set_to_none=False)) need none of it."""
+        p, _, old = self.params.tensors
+        self._take(p, g, old if copies is None else copies)
 
     def step(self, lr: float) -> Optional[torch.Tensor]:
         """One step from the gradients that are in place.  With max_norm: float32 [2] on the device, the gradients'
         norm and the factor they were multiplied by, overwritten by the next step."""
+        for w, d in self._own:
+            if w.grad is not d:
+                raise ValueError("AdamW: a listed gradient is no longer its weight's .grad; renew() takes the new ones")
         norm, k = None, self.steps + 1
         if self.max_norm is not None:
             norm = self._norm
@@ -249,6 +271,13 @@ class AdamW:
         desc = B.make_adamw_desc(lr, k, seed=(self.seed << 40) + k, **self.hyper)
         B.strata_adamw(desc, self.params, self.m, self.v, self.m_scales, self.v_scales, None if norm is None else norm[1:])
         self.steps = k   # a step that was refused is none
+        # a list that renew replaces is let go, but not under a graph, nor before another stream's kernels have read it
+        if torch.cuda.is_current_stream_capturing():
+            if not self._captured or self._captured[-1][0] is not self.params:
+                self._captured.append((self.params, self._ws))
+        elif B._on_gpu(self.params.index, None) != self._stream:
+            for t in (self.params.table, self._ws):
+                t.record_stream(torch.cuda.current_stream(self.params.device))
         return norm
 
     def moments(self, i: int):

@@ -208,3 +208,68 @@ def test_the_scale_of_a_module(dtype):
         out += [y, total, dres, dscale.view(-1)]
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_gradients_allocated_anew(eight):
+    """Gradients set to None and computed again every step, given to renew, against the same values in tensors that stay."""
+    g = gen(21)
+    shapes = [(40, 33), (33,), (7,), (2049,)]
+    first = [0.1 * torch.randn(s, generator=g) for s in shapes]
+    p = [torch.nn.Parameter(x.cuda()) for x in first]
+    q, fixed = [x.cuda() for x in first], [torch.zeros(s, device="cuda") for s in shapes]
+    copies = [torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in shapes]
+    kw = dict(HYPER, eight_bit=eight, max_norm=1.0, seed=4)
+    opt, want, old = None, pipeline.AdamW(q, fixed, **kw), []
+    for k in range(5):
+        for w in p:
+            w.grad = None
+        for i, w in enumerate(p):
+            d = (1e-2 * torch.randn(shapes[i], generator=g)).cuda()
+            (w * d).sum().backward()
+            fixed[i].copy_(d)
+        grads = [w.grad for w in p]
+        if opt is None:
+            opt = pipeline.AdamW(p, grads, copies, **kw)
+        else:
+            with pytest.raises(ValueError, match="renew"):
+                opt.step(1e-3)
+            opt.renew(grads)
+        old.append(grads)                                   # kept, so that the next ones lie elsewhere
+        assert torch.equal(opt.step(1e-3), want.step(1e-3))
+        for a, b, c in zip(p, q, copies):
+            assert torch.equal(a, b) and torch.equal(c, b.bfloat16())
+    assert opt.steps == 5 and torch.equal(opt.m, want.m) and torch.equal(opt.v, want.v)
+
+
+def test_renewed_lists_on_another_stream_and_in_a_graph():
+    """Steps on a stream that the lists were not made on, renewed at once; a captured step keeps the list it was captured
+    with."""
+    g = gen(22)
+    first = 0.1 * torch.randn(300000, generator=g)
+    grads = [(1e-2 * torch.randn(300000, generator=g)).cuda() for _ in range(4)]
+    p, q, d = first.cuda(), first.cuda(), grads[0].clone()
+    opt, want = (pipeline.AdamW([w], [x], **dict(HYPER, max_norm=1.0)) for w, x in ((p, grads[0]), (q, d)))
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for k in range(12):
+        d.copy_(grads[k % 4])
+        want.step(1e-3)
+        opt.renew([grads[k % 4]])
+        with torch.cuda.stream(s):
+            opt.step(1e-3)
+    torch.cuda.synchronize()
+    assert torch.equal(p, q) and torch.equal(opt.m, want.m)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(1e-3)                                      # of grads[3]
+    opt.renew([grads[0]])
+    fill = [torch.zeros(1 << 14, dtype=torch.uint8, device="cuda") for _ in range(64)]   # where a freed list would lie
+    d.copy_(grads[3])
+    want.step(1e-3)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(p, q) and torch.equal(opt.v, want.v) and not any(bool(t.any()) for t in fill)
+    d.copy_(grads[0])
+    want.step(1e-3), opt.step(1e-3)
+    assert torch.equal(p, q) and opt.steps == want.steps == 14

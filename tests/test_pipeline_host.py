@@ -34,6 +34,9 @@ class Host:
         self.steps, self.refuse = [], False
         for name in ("make_params", "strata_grad_norm_workspace_size", "strata_grad_norm", "strata_adamw"):
             monkeypatch.setattr(B, name, getattr(self, name))
+        monkeypatch.setattr(pipeline, "_current_stream", lambda device: 0, raising=False)
+        monkeypatch.setattr(B, "_on_gpu", lambda index, stream: 0)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
 
     def make_params(self, p, g, copies=None):
         made = B.Params((list(p), list(g), copies), B.ParamList(0, len(p), len(p), 32 * len(p)),
@@ -63,3 +66,58 @@ def test_a_refused_step_is_not_counted(monkeypatch):
     host.refuse = False
     opt.step(1e-3)
     assert opt.steps == 2 and [k for k, _, _ in host.steps] == [1, 2] and host.steps[0][1] != host.steps[1][1]
+
+
+def loss(p, k):
+    return sum(((i + k) * w).sum() for i, w in enumerate(p))
+
+
+def test_gradients_allocated_anew(monkeypatch):
+    """A loop whose zero_grad sets gradients to None: a step on the list's old ones is refused, and none is counted;
+    renew takes the new ones and keeps states and steps."""
+    host = Host(monkeypatch)
+    p = [torch.nn.Parameter(torch.ones(4)) for _ in range(3)]
+    loss(p, 1).backward()
+    opt = pipeline.AdamW(p, [w.grad for w in p], seed=5)
+    states = opt.m, opt.v
+    opt.step(1e-3)
+    loss(p, 1).backward()                      # added in place: the same tensors
+    opt.step(1e-3)
+    for fresh in (False, True):                # set to None and not computed again; computed again
+        for w in p:
+            w.grad = None
+        if fresh:
+            loss(p, 2).backward()
+        with pytest.raises(ValueError, match="renew"):
+            opt.step(1e-3)
+    assert opt.steps == 2 and len(host.steps) == 2
+    opt.renew([w.grad for w in p])
+    opt.step(1e-3)
+    assert opt.steps == 3 and opt.m is states[0] and opt.v is states[1] and opt.params.tensors[0] == p
+    assert all(a is w.grad for a, w in zip(host.steps[2][2], p)) and [k for k, _, _ in host.steps] == [1, 2, 3]
+    # gradients that are not the weights' own are the caller's to fill
+    mine = [torch.zeros(4) for _ in p]
+    opt.renew(mine)
+    p[0].grad = None
+    opt.step(1e-3)
+    assert host.steps[3][2] == mine
+    # one without a gradient this time
+    opt.renew([mine[0], None, mine[2]], copies=[None] * 3)
+    opt.step(1e-3)
+    assert host.steps[4][2][1] is None and opt.steps == 5
+
+
+def test_a_list_that_is_refused_leaves_the_old_one(monkeypatch):
+    host = Host(monkeypatch)
+    g = [torch.zeros(4)]
+    opt = pipeline.AdamW([torch.zeros(4)], g)
+    old = opt.params
+
+    def refuse(*args):
+        raise ValueError("refused")
+    monkeypatch.setattr(B, "make_params", refuse)
+    with pytest.raises(ValueError, match="refused"):
+        opt.renew([torch.zeros(5)])
+    assert opt.params is old
+    opt.step(1e-3)
+    assert host.steps[0][2] == g
