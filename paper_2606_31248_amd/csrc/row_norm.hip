@@ -522,20 +522,31 @@ struct Shape {
   int lanes, pieces, threads, teams;
 };
 static bool ragged(const NormArgs& a, bool bf16) { return a.width % (bf16 ? 8 : 4); }
-// Ragged rows, of a wave's piece at most, that are too few to fill the card with a wave a SIMD.
-static bool few(const NormArgs& a, bool bf16) { return ragged(a, bf16) && a.width <= 512 && a.rows < 1 << 16; }
+
+constexpr int kCus = 256;
+constexpr int kWave = 64 * 8;  // channels of a wave's piece
+
+// Lanes of a row of `pieces` a lane: 8 lanes hold the float32 values of a group of codes.
+static int lanes_of(int width, int pieces) {
+  int lanes = width % 32 ? 1 : 8;
+  while (lanes < 64 && lanes * 8 * pieces < width) lanes *= 2;
+  return lanes;
+}
+
+// Ragged rows, of a wave's piece at most, of which the backward's 512 blocks take less than 32 turns with a piece a lane.
+static bool few(const NormArgs& a, bool bf16) {
+  return ragged(a, bf16) && a.width <= kWave && a.rows < 32ll * 2 * kCus * kWaves * 64 / lanes_of(a.width, 1);
+}
 
 static Shape shape_of(const NormArgs& a, bool bf16, bool back) {
-  constexpr int kWave = 64 * 8;  // channels of a wave's piece
   const int width = a.width;
   if (width > 2 * kWave) return {64, 2, 64 * ((width + 2 * kWave - 1) / (2 * kWave)), 1};
   // Two pieces a lane in the backward where rows are long enough for 8 lanes: half as many exchanges an element, and a
   // wave has twice as much in flight.  The forward has more waves in flight instead (rows of 512: 6.5 and 6.2 TB/s), and
-  // so do few ragged rows (15876 of 203 in float32 21.2 us with two pieces and 256 blocks, 18.9 with one and 512; of 999,
-  // which take two anyway, 42.6 and 43.6).
-  const int most = width > 64 && back && !few(a, bf16) ? 2 : 1;
-  int lanes = width % 32 ? 1 : 8;  // 8 lanes hold the float32 values of a group of codes
-  while (lanes < 64 && lanes * 8 * most < width) lanes *= 2;
+  // so do few ragged rows, whose launch is short (us of the backward with one piece and with two, 512 blocks, bf16 but where
+  // said: 2^16 rows of 203 24.2, 24.5, with a gate 33.9, 35.4, in float32 61.3, 67.8; 2^17 of 100 with a gate 32.3, 34.5; 2^15
+  // of 501 38.8, 40.2; but 2^18 of 203 102, 90, 2^17 of 333 96.9, 77.3, 2^19 of 100 82.6, 83.5).
+  const int pieces = width > 64 && back && !few(a, bf16) ? 2 : 1, lanes = lanes_of(width, pieces);
   return {lanes, lanes * 8 < width ? 2 : 1, kWaves * 64, kWaves * 64 / lanes};
 }
 
@@ -552,18 +563,19 @@ static int64_t fwd_blocks(const NormArgs& a, bool bf16) {
 // many.  A wave a SIMD where a wave takes rows (training tile, TB/s with 256, 512, 1024 blocks: 6.4, 5.8, 5.5; with a
 // gate 5.9, 5.0, 5.4), two where waves wait for each other at barriers (rows of 2048: 3.6, 5.5, 6.1) but with a gate's
 // two more streams and three sums (rows of 4096 5.9, 5.5, 5.3).  If rows are many, ragged ones two (rows of 201: 4.3,
-// 5.0, 4.8) or, short ones with a piece a lane, four (rows of 33: 2.4, 3.2, 4.2), and gated ones of float32 four (5.2,
-// 5.7, 6.0).
-constexpr int kCus = 256;
+// 5.0, 4.8) or, short ones with a piece a lane, four (2^20 rows of 33 in bf16: 108, 81, 65 us), and gated ones of float32
+// four (5.2, 5.7, 6.0).  Ragged ones of a wave's piece at most two at the least (with 256 and 512 blocks 2^17 rows of 33 in
+// bf16 18.6 and 15.9 us, 2^16 of 100 17.1 and 16.6, 2^17 of 61 in float32 24.0 and 24.6); wider ones not (2^12 rows of 999
+// in float32 with a gate 24.0 and 29.2).
 static int64_t bwd_blocks(const NormArgs& a, bool bf16, bool all) {
   const Shape at = shape_of(a, bf16, true);
   if (at.teams == 1) {
     const int waves = at.threads / 64, want = all ? 4 : 8;
     return waves >= want ? kCus : kCus * (want / waves);
   }
-  if (few(a, bf16)) return 2 * kCus;
-  const int want = ragged(a, bf16) ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1;
-  return a.rows >= (int64_t)kCus * want * 8 * at.teams ? kCus * want : kCus;
+  const bool off = ragged(a, bf16);
+  const int want = off ? (a.width > 64 ? 2 : 4) : all && !bf16 ? 4 : 1, least = off && a.width <= kWave ? 2 : 1;
+  return kCus * (a.rows >= (int64_t)kCus * want * 8 * at.teams ? want : least);
 }
 
 static int64_t chunks_of(const NormArgs& a, bool bf16, bool all) {

@@ -82,6 +82,17 @@ def test_norm_workspace():
         assert B.strata_residual_norm_bwd_workspace_size(d) <= max(16 << 20, rows * width), (rows, groups, width)
 
 
+@pytest.mark.parametrize("dtype", [B.STRATA_BF16, B.STRATA_F32])
+def test_more_rows_take_no_fewer_blocks(dtype):
+    """A block of the backward is a row of partial sums in the workspace: as rows of a width grow its size never falls."""
+    for width in list(range(1, 140)) + [203, 255, 257, 333, 501, 511, 513, 768, 999, 1024, 1293, 2048, 4096, 8192]:
+        last = 0
+        for rows in sorted({(1 << k) + d for k in range(0, 21) for d in (-1, 0, 1)} - {0}):
+            size = B.strata_residual_norm_bwd_workspace_size(desc(rows=rows, group_rows=rows, width=width, dtype=dtype))
+            assert size >= last, (width, rows)
+            last = size
+
+
 # ---- lists of weights ----------------------------------------------------------------
 
 def entries(*tensors):
