@@ -360,7 +360,7 @@ strata_status strata_ckpt_unpack(const int8_t* codes, const uint8_t* scales, int
  * sum may be res or x itself; no other buffers may overlap. */
 typedef struct {
   int64_t rows;       /* 1 to 2^31 - 1, rows * width below 2^40 */
-  int64_t group_rows; /* divides rows */
+  int64_t group_rows; /* divides rows; a block of the backward takes rows of one group, so groups of few are slow */
   int32_t width;      /* 1 to 8192; whole 16 bytes of dtype are fastest */
   float eps;          /* finite, >= 0 */
   strata_dtype dtype; /* x, res, sum, y and the gradients of the rows */
@@ -374,8 +374,9 @@ strata_status strata_residual_norm(const strata_norm_desc* desc, const void* x, 
  * 0).  sum: the forward's (without x: its res).  With n = r sum, u = r scale dy:
  *   dres = u - n mean_c(u_c n_c) + dsum,            dx = gate dres,
  *   dscale = sum_t dy n,   dshift = sum_t dy,       dgate = sum_t dres x,
- * sums over the rows t of a group, in float32 in a fixed order (deterministic); dres and dx
- * rounded once, dgate of the unrounded dres.  Without a gate dx is dres (pass NULL); with
+ * sums over the rows t of a group, in float32 in a fixed order (deterministic), off by at most
+ * (rows / 128 + 512) 2^-24 of the sum of their terms' magnitudes, for up to 1024 channels
+ * (rows / 800 + 512) 2^-24; dres and dx rounded once, dgate of the unrounded dres.  Without a gate dx is dres (pass NULL); with
  * one x, dx and dgate are needed.  dscale: needed with scale, NULL without; dshift: NULL if
  * it is not wanted.  dgate, dscale, dshift: float32 [rows / group_rows, width], written.
  * workspace: at least strata_residual_norm_bwd_workspace_size(desc) bytes (may be 0) where
@@ -421,7 +422,8 @@ strata_status strata_params_table(const strata_param* tensors, int64_t count, vo
  * min(1, max_norm / N): what clips them (1 for N = 0; NaN where a gradient is not finite).
  * norm: float32 [2] on the device.  Sums in float64 in a fixed order; no gradient is too
  * large or small for it (norm[0] itself rounds to float32).  max_norm > 0, infinity: no
- * clipping.  workspace: strata_grad_norm_workspace_size(params) bytes (may be 0). */
+ * clipping.  workspace: strata_grad_norm_workspace_size(params) bytes (may be 0); calls in
+ * flight at once need one each. */
 size_t strata_grad_norm_workspace_size(const strata_params* params);
 strata_status strata_grad_norm(const strata_params* params, double max_norm, float* norm, void* workspace,
                                size_t workspace_bytes, void* stream);

@@ -403,3 +403,29 @@ def test_refusals():
     B.strata_residual_norm(single.desc, None, None, single.res, single.scale[0], None, None, y)   # one group: [width] too
     assert torch.equal(y, single.forward()["y"])
     c.guards()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(1 << 20, 24), ((1 << 21) + 77, 5), (1 << 19, 33), (1 << 14, 1100)])
+def test_sums_over_many_rows(rows, width, dtype):
+    """The vectors' gradients as the header bounds them: a lane adds at most rows / 800 terms one after the other (of
+    more than 1024 channels rows / 128), each within 128 2^-24, and the rest is trees and short chains.  Terms of one
+    sign, so that the partial sums grow as large as the bound's magnitudes; 64 bits on the device."""
+    per = 800 if width <= 1024 else 128
+    tol = (rows / per + 512) * 2.0 ** -24
+    c = Norm(dtype, 1, rows, width, "x gate scale dsum")
+    for t in (c.res, c.x, c.dy, c.dsum):
+        t.abs_().add_(0.5)
+    c.gate.abs_()
+    out = c.forward()
+    g = c.backward(out["sum"])
+    c.guards()
+    total, dy = out["sum"].double(), c.dy.double()
+    n = total / (total.square().mean(1, keepdim=True) + EPS).sqrt()
+    u = dy * c.scale.double() * (n / total)
+    h = u - n * (u * n).mean(1, keepdim=True) + c.dsum.double()
+    mag = u.abs() + n.abs() * (u * n).abs().mean(1, keepdim=True) + c.dsum.double()
+    x = c.x.double()
+    for name, want, size in (("dscale", dy * n, dy * n), ("dshift", dy, dy), ("dgate", h * x, mag * x)):
+        off = (g[name].double() - want.sum(0, keepdim=True)).abs() / size.abs().sum(0, keepdim=True)
+        assert float(off.max()) <= tol, (name, float(off.max()), tol)
