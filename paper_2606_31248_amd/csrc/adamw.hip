@@ -2,8 +2,8 @@
 //
 // Every element is read and written once: 28 bytes with states in 32 bits, bf16 gradients
 // and a bf16 copy, 16 with states in 8.  HBM bounds the first (all weights of 24 blocks of
-// 1024 channels: 1520 us, 6.0 TB/s of 6.5 that a copy reaches); the second takes 83 vector
-// instructions an element beside it, two thirds of its time (865 us, 6.1 TB/s).  A block takes kParamChunk elements of one
+// 1024 channels: 1525 us, 6.0 TB/s of 6.5 that a copy reaches); the second takes 83 vector
+// instructions an element beside it, two thirds of its time (873 us, 6.0 TB/s).  A block takes kParamChunk elements of one
 // tensor; a lane 4 neighbouring ones at a time, 16 bytes of float32, so that 8 lanes hold a
 // group of the 8-bit states.
 #include "state8.h"
@@ -25,8 +25,8 @@ __device__ __forceinline__ Global<T> global(P* p) {
   return (Global<T>)reinterpret_cast<uintptr_t>(p);
 }
 
-// 16, 8 or 4 bytes that are touched once a step, past the caches' replacement (those weights 1547 us, through the
-// caches 1707; 300 tensors of 5.4 million weights 18.3 and 18.5).
+// 16, 8 or 4 bytes that are touched once a step, past the caches' replacement (those weights 1525 us, through the
+// caches 1685; 300 tensors of 5.4 million weights in 8 bits 17.7 and 18.6).
 template <typename T>
 __device__ __forceinline__ T load(Global<const T> p) {
   return __builtin_nontemporal_load(p);
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const AdamArgs a) {
   if (factor != factor) return;  // gradients that are not finite: nothing changes
   const ParamRecord t = a.tensors[a.owner[chunk]];
   const int64_t base = (chunk - t.chunk) * kParamChunk;
-  // without the checks 8 bits take 865 us instead of 925 (24 blocks of 1024 channels), 32 bits 1550 instead of 1518
+  // without the checks 8 bits take 873 us instead of 922 (24 blocks of 1024 channels), 32 bits 1549 instead of 1525
   if (EIGHT && base + kParamChunk <= t.n)
     step_chunk<EIGHT, true>(a, t, base + 4 * threadIdx.x, factor);
   else

@@ -110,7 +110,7 @@ void launch_residual_norm_bwd(NormArgs a, strata_dtype dt, hipStream_t s);
 
 // AdamW over many tensors (adamw.hip).  The table on the device: one record a tensor, then the
 // tensor's index for every chunk of kParamChunk elements of the tensors with a gradient.
-constexpr int kParamChunk = 1024;  // 32-bit states 1548 us, with 2048 1603 and 4096 1619; in 8 bits no difference
+constexpr int kParamChunk = 1024;  // 32-bit states 1525 us, with 2048 1613 and 4096 1650; in 8 bits 873, 858, 867
 struct ParamRecord {
   float* p;
   const void* g;

@@ -1,7 +1,7 @@
 // The residual stream's addition with its RMS norm, and the gradients.
 //
-// Both directions stream: a bf16 element costs 8 bytes forward (10 to 12 backward) and
-// about 10 (20) operations, so HBM bounds them.  A lane holds 8 channels of a piece of
+// Both directions stream: a bf16 element costs 8 bytes forward (backward 6 to 8, with a gate
+// 10 to 12) and about 10 (20) operations, so HBM bounds them.  A lane holds 8 channels of a piece of
 // 8 * LANES, a team of LANES lanes PIECES of them, so that a row is read once and stays in
 // registers between its statistics and its results; rows wider than one wave are shared by
 // the waves of a block, which add their sums in LDS.  Training tile (2^18 rows of 1024 in
@@ -582,7 +582,8 @@ static int64_t chunks_of(const NormArgs& a, bool bf16, bool all) {
   const int teams = shape_of(a, bf16, true).teams;
   const int64_t most = (a.group_rows + teams - 1) / teams;
   if (most <= 4) return 1;  // a second launch would take longer
-  // partial sums of 16 MiB, or a block's for 12 rows, a tenth of what these move in bf16
+  // partial sums of 16 MiB, or a block's for 12 rows: of three vectors a byte an element, of the 6 to 12 that these move
+  // in bf16
   const int64_t room = std::max<int64_t>((16 << 20) / (3 * 4 * a.width), a.rows / 12);
   const int64_t fill = std::min(room, bwd_blocks(a, bf16, all));
   // as many for each group as fit, or one more where a fifth of the card would be idle

@@ -231,7 +231,8 @@ class AdamW:
     are.  Gradients that are allocated anew, as where zero_grad sets them to None, are given to `renew` before the step
     that takes them: a list of weights' own .grad refuses a step on one that was replaced.  m, v and, in 8 bits, m_scales
     and v_scales are the states, flat, and `steps` the steps taken: what a checkpoint stores.  A step whose gradients
-    are not all finite changes no tensor if it clips (max_norm, which may be infinity), but is counted."""
+    are not all finite changes no tensor if it clips (max_norm, which may be infinity), but is counted.  A captured step
+    repeats its learning rate, its number and its seed."""
 
     def __init__(self, p, g, copies=None, eight_bit: bool = False, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, weight_decay: float = 0.0, max_norm: Optional[float] = None, seed: int = 0):
