@@ -784,10 +784,10 @@ def make_params(p, g, copies=None) -> Params:
             _need(f"p[{i}]", w, None, f32, None if index < 0 else torch.device("cuda", index))
         kind = STRATA_F32
         if d is not None:
-            kind = STRATA_BF16 if type(d) in tensors and d.dtype is bf16 else STRATA_F32
+            kind = STRATA_BF16 if getattr(d, "dtype", f32) is bf16 else STRATA_F32
             if not (type(d) in tensors and (kind == STRATA_BF16 or d.dtype is f32) and d.get_device() == index
                     and d.shape == w.shape and d.is_contiguous()):
-                _need(f"g[{i}]", d, w.shape, f32, w.device)
+                _need(f"g[{i}]", d, w.shape, bf16 if kind == STRATA_BF16 else f32, w.device)
         if c is not None and not (type(c) in tensors and c.dtype is bf16 and c.get_device() == index
                                   and c.shape == w.shape and c.is_contiguous()):
             _need(f"copies[{i}]", c, w.shape, bf16, w.device)

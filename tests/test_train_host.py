@@ -315,6 +315,19 @@ def test_vectors_of_a_single_group(launches):
             forward(scale=torch.Tensor._make_subclass(kind, torch.zeros(64)))
 
 
+def test_what_a_list_says_of_a_gradient(monkeypatch):
+    """A gradient in bf16 is one, of whatever class and shape: what is wrong with it is named."""
+    w = torch.Tensor._make_subclass(OnGpu, torch.zeros(4, 8))
+    for dtype in (torch.bfloat16, torch.float32):
+        with pytest.raises(ValueError, match="shape"):
+            B.make_params([w], [on_gpu((4, 7), dtype)])
+    with pytest.raises(ValueError, match="dtype"):
+        B.make_params([w], [on_gpu((4, 8), torch.float16)])
+    monkeypatch.setattr(B, "load", lambda: (_ for _ in ()).throw(RuntimeError("the list was accepted")))
+    with pytest.raises(RuntimeError, match="accepted"):
+        B.make_params([w], [on_gpu((4, 8))])
+
+
 # ---- the oracle ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("second", [False, True])
