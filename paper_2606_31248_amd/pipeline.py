@@ -249,15 +249,21 @@ class AdamW:
     def _take(self, p, g, copies):
         params = B.make_params(p, g, copies)
         ws = torch.empty(B.strata_grad_norm_workspace_size(params), dtype=torch.uint8, device=params.device)
-        self.params, self._ws, self._stream = params, ws, _current_stream(params.device)
+        self.params, self._ws = params, ws
+        self._stream, self._others = _current_stream(params.device), {}  # of the list, and of steps elsewhere
         self._own = [(w, d) for w, d in zip(*params.tensors[:2]) if d is not None and w.is_leaf and w.grad is d]
 
     def renew(self, g, copies=None):
         """Other gradients (None: that tensor is left as it is) and copies (default: the present ones) from the next step
         on; weights, states and steps stay.  Makes the list's table and copies it to the device, 0.4 ms for 300 tensors:
         gradients that stay where they are (zero_grad(set_to_none=False)) need none of it."""
-        p, _, old = self.params.tensors
-        self._take(p, g, old if copies is None else copies)
+        p, *old = self.params.tensors
+        others = self._others.values()
+        self._take(p, g, old[1] if copies is None else copies)
+        for s in others:  # let go once these streams have read them
+            for t in old[0] + old[1]:
+                if t is not None:
+                    t.record_stream(s)
 
     def step(self, lr: float) -> Optional[torch.Tensor]:
         """One step from the gradients that are in place.  With max_norm: float32 [2] on the device, the gradients'
@@ -276,9 +282,12 @@ class AdamW:
         if torch.cuda.is_current_stream_capturing():
             if not self._captured or self._captured[-1][0] is not self.params:
                 self._captured.append((self.params, self._ws))
-        elif B._on_gpu(self.params.index, None) != self._stream:
+            return norm
+        stream = B._on_gpu(self.params.index, None)
+        if stream != self._stream:
+            s = self._others[stream] = torch.cuda.current_stream(self.params.device)
             for t in (self.params.table, self._ws):
-                t.record_stream(torch.cuda.current_stream(self.params.device))
+                t.record_stream(s)
         return norm
 
     def moments(self, i: int):

@@ -273,3 +273,28 @@ def test_renewed_lists_on_another_stream_and_in_a_graph():
     d.copy_(grads[0])
     want.step(1e-3), opt.step(1e-3)
     assert torch.equal(p, q) and opt.steps == want.steps == 14
+
+
+def test_gradients_let_go_while_another_stream_waits_to_read_them():
+    """A step on another stream, behind work that takes longer than the host: renewed at once, its gradients' memory is
+    not given to others before the step has read them."""
+    g = gen(23)
+    n = 1 << 20
+    grads = [1e-2 * torch.randn(n, generator=g) for _ in range(3)]
+    p, q = (torch.ones(n, device="cuda") for _ in range(2))
+    want = pipeline.AdamW([q], [torch.empty_like(q)], **HYPER)
+    opt = pipeline.AdamW([p], [grads[0].cuda()], **HYPER)
+    busy, s = torch.randn(4096, 4096, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for k in range(3):
+        want.params.tensors[1][0].copy_(grads[k])
+        want.step(1e-3)
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                busy @ busy
+            opt.step(1e-3)
+        opt.renew([grads[(k + 1) % 3].cuda()])
+        fill = [torch.full((n,), 1e3, device="cuda") for _ in range(4)]   # where the gradients lay, if it were free
+        torch.cuda.synchronize()
+        assert torch.equal(p, q) and torch.equal(opt.m, want.m), k
+        del fill

@@ -121,3 +121,29 @@ def test_a_list_that_is_refused_leaves_the_old_one(monkeypatch):
     assert opt.params is old
     opt.step(1e-3)
     assert host.steps[0][2] == g
+
+
+def test_gradients_that_another_stream_still_reads(monkeypatch):
+    """What renew lets go is marked for the streams that steps ran on beside the list's own, and only then."""
+    host, now, marked = Host(monkeypatch), [0], []
+    monkeypatch.setattr(B, "_on_gpu", lambda index, stream: now[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: marked.append((t, s)))
+    first, second, third = ([torch.zeros(4), None] for _ in range(3))
+    opt = pipeline.AdamW([torch.zeros(4), torch.zeros(2)], first, [None, torch.zeros(2, dtype=torch.bfloat16)])
+    copy = opt.params.tensors[2][1]
+    opt.step(1e-3)
+    opt.renew(second)
+    assert not marked
+    table = opt.params.table
+    now[0] = 5
+    opt.step(1e-3), opt.step(1e-3)
+    assert marked and all(s == 5 for _, s in marked) and any(t is table for t, _ in marked)
+    now[0] = 0
+    marked.clear()
+    opt.renew(third)
+    assert [s for _, s in marked] == [5, 5] and marked[0][0] is second[0] and marked[1][0] is copy
+    marked.clear()
+    opt.step(1e-3)
+    opt.renew(first)
+    assert not marked and len(host.steps) == 4
